@@ -243,9 +243,9 @@ def prepare(c, seed: int) -> dict:
             s["pool"] = llmig.Pool(list(s["kv"][0].unbind(0)), list(s["kv"][1].unbind(0)), s["layouts"])
         if "bounds" in s:
             s["bounds_pool"] = llmig.Pool(list(s["bounds"][0].unbind(0)), list(s["bounds"][1].unbind(0)))
-        need = {"select": lambda: llmig.select_workspace_bytes(after, bs, L, H),
-                "blocks": lambda: llmig.decode_blocks_workspace_bytes(after, bs, c["count"], L, H * G, D),
-                "prefix": lambda: llmig.decode_prefix_workspace_bytes(after, bs, shared, L, H * G, D)}
+        need = {"select": lambda: llmig.select_workspace_bytes(s["bounds_pool"], bs, after),
+                "blocks": lambda: llmig.decode_blocks_workspace_bytes(s["pool"], after, H * G, c["count"]),
+                "prefix": lambda: llmig.decode_prefix_workspace_bytes(s["pool"], after, H * G, shared)}
         if c["kind"] in need:
             s["ws"] = torch.empty(max(16, need[c["kind"]]()), dtype=torch.uint8, device="cuda")
     return s
