@@ -450,6 +450,126 @@ int llmig_decode_attention_noalloc(const llmig_pool *pool, int32_t dtype, const 
                                    int32_t q_heads, const int32_t *tables, int32_t table_stride,
                                    const int32_t *ctx_lens, float scale, float *out, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * A decode step over long contexts, on the pools above: new tokens enter the
+ * cache with their rotation applied (llmig_append_rotary), the bounds of the
+ * blocks' keys follow (llmig_key_bounds), a cheap score chooses blocks for each
+ * sequence and KV head (llmig_select_blocks) and attention reads those alone
+ * (llmig_decode_attention_blocks); a batch behind one shared prefix has it read
+ * once (llmig_decode_attention_prefix).  All of them: 16-bit pools (dtype 0
+ * fp16, 1 bf16), batch <= 256, tables device int32 [batch][table_stride] whose
+ * ids the caller guarantees in range (an id outside the pool is never written
+ * to), host arrays of lengths that may be reused as soon as the call returns.
+ * They allocate nothing, so they may be captured into a HIP graph (with the
+ * lengths of the captured call).  Results do not change from call to call.
+ * ------------------------------------------------------------------------- */
+
+/* New tokens of a batch.  Sequence b appends n_toks[b] tokens (0 is allowed) at
+ * from_toks[b] of its own; their rows follow each other in sequence order, n
+ * rows in all.  Row j of layer l of q, k and v starts layer * l + token * j
+ * elements behind the array's address, heads by heads ([q_heads][head_dim], or
+ * [num_kv_heads][head_dim]), so the arrays may be slices of one projection's
+ * output.  Addresses and strides: 16-byte multiples, strides not negative. */
+typedef struct llmig_append_desc {
+    int32_t dtype;
+    int32_t batch;
+    int32_t q_heads;          /* 0: no queries (q and q_out are not read) */
+    int32_t table_stride;
+    const void *q, *k, *v;    /* device */
+    void *q_out;              /* device [num_layers][n][q_heads][head_dim], apart from q, k and v */
+    int64_t q_layer, q_token, k_layer, k_token, v_layer, v_token;
+    const int32_t *tables;    /* device */
+    const int32_t *from_toks; /* host */
+    const int32_t *n_toks;    /* host */
+    const int32_t *first_pos; /* host: position of each sequence's first new token; NULL: from_toks */
+    const float *cos_sin;     /* device [positions][rotary_dim]: rotary_dim / 2 cosines, then as many sines */
+    int32_t positions;
+    int32_t rotary_dim;       /* even, at most head_dim; 0: nothing is rotated, cos_sin is not read */
+    int32_t interleaved;      /* 0: pairs (i, i + rotary_dim / 2); 1: pairs (2i, 2i + 1) */
+} llmig_append_desc;
+
+/* Writes the new tokens' keys, rotated, and values, as they are, into the pool
+ * (any layout; the slots of llmig_write_tokens), and the queries, rotated, into
+ * q_out.  A pair (x, y) at angle a becomes (x cos a - y sin a, y cos a + x sin
+ * a), in fp32, rounded once (nearest even) to the pool's type; dims from
+ * rotary_dim on stay as they are.  elem_bytes == 2, head_dim % 8 == 0, and
+ * distinct slots (no two sequences append to one block's same slot; the
+ * caller's guarantee).  LLMIG_EINVAL for a bad size, alignment, table_stride too
+ * short for a sequence's last token, or a position outside the table. */
+int llmig_append_rotary(const llmig_pool *pool, const llmig_append_desc *desc, void *stream);
+
+/* Brings the bounds of the keys up to date after tokens [from_toks[b],
+ * ctx_lens[b]) of each sequence were written: of every block that holds one of
+ * them, the least and the largest value of each (layer, KV head, dim) over the
+ * block's tokens (those before ctx_lens[b]).  bounds is a pool of its own, of
+ * the same layers, blocks, heads, head_dim and type and of block_size 1: its K
+ * tiles hold the least, its V tiles the largest values, block by block, so
+ * llmig_stage, llmig_pack and llmig_unpack migrate them with the cache's own
+ * block maps.  A NaN key makes its two bounds NaN.  Blocks that other sequences
+ * of the call update as well (a shared prefix) get the same values from each
+ * that holds all of their tokens.  Both pools NHD, head_dim % 8 == 0; 0 <=
+ * from_toks[b] <= ctx_lens[b]; else LLMIG_EINVAL. */
+int llmig_key_bounds(const llmig_pool *pool, const llmig_pool *bounds, int32_t dtype, int32_t batch,
+                     const int32_t *tables, int32_t table_stride, const int32_t *from_toks,
+                     const int32_t *ctx_lens, void *stream);
+
+/* Chooses blocks for each (layer, sequence b, KV head g) by what their bounds
+ * allow a score to reach.  With q device [num_layers][batch][q_heads][head_dim]
+ * (16-byte aligned) and a sequence of n = ceil(ctx_lens[b] / block_size) blocks:
+ *     score_j = sum_d P_d hi_jd + N_d lo_jd,   P_d = sum_h max(q_hd, 0),  N_d = sum_h min(q_hd, 0)
+ * over the query heads h of g, the sum over them of the largest q_h . k that
+ * keys within the block's bounds can have.  Sums in 64 bits; a NaN score counts
+ * as +infinity.  The first keep_first and the last keep_last blocks are always
+ * chosen, then those of the highest scores (of equal ones the first), `count`
+ * in all, or all n where n <= count.  blocks: device int32
+ * [num_layers][batch][num_kv_heads][count], the chosen block numbers (indexes
+ * into the sequence's table row) ascending, then -1.  count >= 1 and >=
+ * keep_first + keep_last; bounds as llmig_key_bounds keeps them, head_dim 64 or
+ * 128; q_heads a multiple of its heads.  workspace: device memory of the size
+ * that llmig_select_blocks_workspace returns for the same lengths, 8-byte
+ * aligned. */
+int llmig_select_blocks_workspace(const llmig_pool *bounds, int32_t block_size, const int32_t *ctx_lens,
+                                  int32_t batch, int64_t *bytes);
+int llmig_select_blocks(const llmig_pool *bounds, int32_t dtype, int32_t block_size, const void *q, int32_t batch,
+                        int32_t q_heads, const int32_t *tables, int32_t table_stride, const int32_t *ctx_lens,
+                        int32_t keep_first, int32_t keep_last, int32_t count, void *workspace,
+                        int64_t workspace_bytes, int32_t *blocks, void *stream);
+
+/* llmig_decode_attention over listed blocks: (layer l, sequence b, KV head g)
+ * attends to the tokens t < ctx_lens[b] of the blocks that row [l][b][g] of
+ * blocks (device int32 [num_layers][batch][num_kv_heads][count]) names, in any
+ * order.  Of a row the first min(count, ceil(ctx_lens[b] / block_size)) entries
+ * are read; one that is negative or past the sequence's last block counts for
+ * nothing, and a block named twice counts twice.  A row that names no token
+ * gives zeros.  workspace: the size that
+ * llmig_decode_attention_blocks_workspace returns for the same lengths, 16-byte
+ * aligned.  Other arguments, limits, arithmetic and errors as
+ * llmig_decode_attention. */
+int llmig_decode_attention_blocks_workspace(const llmig_pool *pool, const int32_t *ctx_lens, int32_t batch,
+                                            int32_t q_heads, int32_t count, int64_t *bytes);
+int llmig_decode_attention_blocks(const llmig_pool *pool, int32_t dtype, const void *q, int32_t batch,
+                                  int32_t q_heads, const int32_t *tables, int32_t table_stride,
+                                  const int32_t *ctx_lens, const int32_t *blocks, int32_t count, float scale,
+                                  void *workspace, int64_t workspace_bytes, float *out, void *stream);
+
+/* llmig_decode_attention of a batch whose sequences share their first
+ * prefix_blocks blocks (a system prompt, a document, beams): the first
+ * prefix_blocks entries of the table rows are the same, in every sequence that
+ * is at least that long (the caller's guarantee; shorter ones share nothing and
+ * may be empty).  The prefix is read once for all of them instead of once for
+ * each, and its products run on the matrix cores as one of many columns.
+ * Results are those of llmig_decode_attention, sums in another order.
+ * 0 <= prefix_blocks <= table_stride.  workspace: the size that
+ * llmig_decode_attention_prefix_workspace returns for the same lengths and
+ * prefix, 16-byte aligned.  Other arguments, limits and errors as
+ * llmig_decode_attention. */
+int llmig_decode_attention_prefix_workspace(const llmig_pool *pool, const int32_t *ctx_lens, int32_t batch,
+                                            int32_t q_heads, int32_t prefix_blocks, int64_t *bytes);
+int llmig_decode_attention_prefix(const llmig_pool *pool, int32_t dtype, const void *q, int32_t batch,
+                                  int32_t q_heads, const int32_t *tables, int32_t table_stride,
+                                  const int32_t *ctx_lens, int32_t prefix_blocks, float scale, void *workspace,
+                                  int64_t workspace_bytes, float *out, void *stream);
+
 /* Static description of a code; never NULL. */
 const char *llmig_strerror(int code);
 

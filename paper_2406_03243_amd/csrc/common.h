@@ -108,6 +108,12 @@ __device__ __forceinline__ int32_t id_entry(const int32_t *ids, uint32_t k)
     return ((const LLMIG_CONSTANT int32_t *)ids)[k];
 }
 
+// Entry k of row s of the block tables.
+__device__ __forceinline__ uint32_t table_id(const int32_t *tables, uint32_t s, uint32_t stride, uint32_t k)
+{
+    return static_cast<uint32_t>(id_entry(tables + static_cast<uint64_t>(s) * stride, k));
+}
+
 __device__ __forceinline__ u32x4 load16(const uint8_t *p)
 {
     return __builtin_nontemporal_load((const LLMIG_GLOBAL u32x4 *)p);

@@ -73,6 +73,22 @@ struct AttnArgs {
     int32_t dst_blocks;         // blocks of the destination pool
 };
 
+// Attention over listed blocks (attn_partial_mfma, MODE kAttnListed): sequence
+// s stands for the tokens of the first `count` entries, at most, of a list per
+// (layer, sequence, KV head); its ctx is the length of that virtual sequence.
+struct AttnListedArgs : AttnArgs {
+    const int32_t *lists;             // [L][B][H][count], logical blocks
+    uint32_t count, num_blocks;
+    int32_t tokens[kAttnMaxBatch];    // of sequence b (its number in the batch)
+};
+
+// The tokens behind a shared prefix (MODE kAttnOwn): ctx counts those alone,
+// and the tables of the sequences whose bit is set start skip blocks later.
+struct AttnOwnArgs : AttnArgs {
+    uint32_t skip;
+    uint32_t behind[kAttnMaxBatch / 32];
+};
+
 struct AttnReduceArgs {
     const float *ws;
     float *out;                 // [L][B][Hq][D]
@@ -352,10 +368,26 @@ __host__ __device__ inline uint32_t attn_blk_slots(uint32_t part_tokens, uint32_
 // rows of a unit from one lane (v_readlane: a scalar base plus lane offsets
 // that never change).  A partition has at most 64 units per wavefront.  Other
 // block sizes stage the block ids in LDS and look each token's up.
-template <int BF16, int D, int MIG, int UNITS>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(MIG ? 3 : 4, 8)))
-attn_partial_mfma(const AttnArgs a)
+//
+// MODE: what a launch does besides plain attention (MIG: kAttnMigrating).
+//  kAttnListed  each (layer, sequence, KV head) attends to the blocks of a list.
+//               A unit's row lookup goes through the list, and a unit has a
+//               number of rows that hold tokens; the others (an entry that names
+//               no block of the sequence, the last block's free slots) weigh 0,
+//               and their V rows count as zeros, whatever the pool holds there.
+//  kAttnOwn     the tokens of each sequence behind a prefix that prefix_rows
+//               (prefix_attention.h) computes: every item leaves a record.
+enum AttnMode { kAttnPlain = 0, kAttnMigrating = 1, kAttnListed = 2, kAttnOwn = 3 };
+
+template <int MODE> struct AttnArgsOf { typedef AttnArgs type; };
+template <> struct AttnArgsOf<kAttnListed> { typedef AttnListedArgs type; };
+template <> struct AttnArgsOf<kAttnOwn> { typedef AttnOwnArgs type; };
+
+template <int BF16, int D, int MODE, int UNITS>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(MODE == kAttnMigrating ? 3 : 4, 8)))
+attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
 {
+    constexpr bool MIG = MODE == kAttnMigrating, LISTED = MODE == kAttnListed;
     constexpr int KS = D / 32;            // k-steps of the QK product
     constexpr int MT = D / 16;            // 16-dim tiles of the PV product
     constexpr int LPR = D / 8;            // lanes per row in the K and V loads (16 bytes each)
@@ -440,6 +472,26 @@ attn_partial_mfma(const AttnArgs a)
     // sequence's.
     const bool mig = MIG && static_cast<int32_t>(b) == a.mig_seq;
     const int32_t *table = a.tables + static_cast<uint64_t>(b) * a.table_stride;
+    if constexpr (MODE == kAttnOwn)
+        table += a.behind[b / 32u] >> (b % 32u) & 1u ? a.skip : 0u;
+    // LISTED: the list, the block behind its entry e and how many tokens that
+    // block holds (0: the entry names no block of the sequence)
+    const int32_t *list = nullptr;
+    if constexpr (LISTED)
+        list = a.lists + ((static_cast<uint64_t>(layer) * a.batch + b) * a.kv_heads + g) * a.count;
+    auto listed_block = [&](int32_t e, uint32_t *block) {
+        int32_t held = 0;
+        *block = 0;
+        if constexpr (LISTED) {
+            const int32_t j = list[e], n = a.tokens[b];
+            if (j >= 0 && j <= (n - 1) / bs) {
+                // (an id outside the pool, which the caller rules out, reads its last block)
+                *block = min(static_cast<uint32_t>(table[j]), a.num_blocks - 1u);
+                held = min(n - j * bs, bs);
+            }
+        }
+        return held;
+    };
     const int32_t tg0 = start + 16 * static_cast<int32_t>(wv);
     const int32_t first_blk = UNITS ? 0 : start / bs;
     int32_t *sh_dst = sh_blk + attn_blk_slots(a.part_tokens, a.block_size);
@@ -449,11 +501,19 @@ attn_partial_mfma(const AttnArgs a)
     // lands in the destination pool (-1: not in the stage).
     uint32_t unit_slot = 0;
     int32_t unit_dst = -1;
+    int32_t unit_held = 0;     // LISTED: rows of the unit that hold tokens
     if constexpr (UNITS) {
         if (tg0 < end) {
             const int32_t t = min(tg0 + 64 * static_cast<int32_t>(lane / 2) + 8 * static_cast<int32_t>(lane % 2), end - 1);
             const int32_t blk = t / bs;
-            unit_slot = static_cast<uint32_t>(table[blk]) * a.block_size + static_cast<uint32_t>(t - blk * bs);
+            if constexpr (LISTED) {
+                uint32_t block;
+                const int32_t off = t - blk * bs;       // (past the end: the last token's)
+                unit_held = max(min(listed_block(blk, &block) - off, 8), 0);
+                unit_slot = block * a.block_size + static_cast<uint32_t>(off);
+            } else {
+                unit_slot = static_cast<uint32_t>(table[blk]) * a.block_size + static_cast<uint32_t>(t - blk * bs);
+            }
             if (mig && blk >= a.mig_from && blk < a.mig_to) {
                 const int32_t id = a.mig_ids[blk - a.mig_from];
                 if (id >= 0 && id < a.dst_blocks)      // an id outside the pool is not written
@@ -464,8 +524,15 @@ attn_partial_mfma(const AttnArgs a)
         // the partition's block ids, once, and the destination block of each
         // of its logical blocks (-1 outside the stage)
         const int32_t n_blk = end > start ? (end - 1) / bs - first_blk + 1 : 0;
-        for (int32_t k = threadIdx.x; k < n_blk; k += kThreads)
-            sh_blk[k] = table[first_blk + k];
+        for (int32_t k = threadIdx.x; k < n_blk; k += kThreads) {
+            if constexpr (LISTED) {
+                uint32_t block;
+                sh_dst[k] = listed_block(first_blk + k, &block);    // tokens held, where a migration keeps its ids
+                sh_blk[k] = static_cast<int32_t>(block);
+            } else {
+                sh_blk[k] = table[first_blk + k];
+            }
+        }
         if (mig) {
             for (int32_t k = threadIdx.x; k < n_blk; k += kThreads) {
                 const int32_t j = first_blk + k;
@@ -518,7 +585,9 @@ attn_partial_mfma(const AttnArgs a)
                 const uint32_t slot = __builtin_amdgcn_readlane(unit_slot, u0 + half);
                 const uint64_t base = (static_cast<uint64_t>(slot) * a.kv_heads + g) * RB;
                 // rows of the unit that hold tokens of the partition, less one
-                const int32_t last = max(min(end - 1 - (t0 + 8 * half), 7), 0);
+                int32_t last = max(min(end - 1 - (t0 + 8 * half), 7), 0);
+                if constexpr (LISTED)       // rows that hold tokens, as the pool may hold anything in the others
+                    last = max(min(last, static_cast<int32_t>(__builtin_amdgcn_readlane(unit_held, u0 + half)) - 1), 0);
 #pragma unroll
                 for (int i = 0; i < IPU; ++i) {
                     const int j = half * IPU + i;
@@ -631,6 +700,33 @@ attn_partial_mfma(const AttnArgs a)
         u32x4 kf[KS];
         uint64_t vf[MT];
         read_operands<KS, MT>(k_at, v_at, kf, vf);
+        // LISTED: the lane's tokens tg + 4*g4 + i that the sequence holds, as
+        // a bit each; the V rows of the others become zeros (0 * NaN is NaN)
+        uint32_t held = 15u;
+        if constexpr (LISTED) {
+            if constexpr (UNITS) {
+                const uint32_t u0 = static_cast<uint32_t>(tg - tg0) / 32u;
+                const int32_t h0 = static_cast<int32_t>(__builtin_amdgcn_readlane(unit_held, u0)),
+                              h1 = static_cast<int32_t>(__builtin_amdgcn_readlane(unit_held, u0 + 1));
+                const int32_t left = (g4 < 2 ? h0 : h1) - 4 * static_cast<int32_t>(g4 % 2);
+                held = left >= 4 ? 15u : left <= 0 ? 0u : (1u << left) - 1u;
+            } else {
+                held = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int32_t t = min(tg + static_cast<int32_t>(4 * g4) + i, end - 1), e = t / bs;
+                    held |= t - e * bs < sh_dst[e - first_blk] ? 1u << i : 0u;
+                }
+            }
+            if (__ballot(held != 15u)) {
+                const uint64_t lo = (held & 1u ? 0xffffull : 0ull) | (held & 2u ? 0xffff0000ull : 0ull),
+                               hi = (held & 4u ? 0xffffull : 0ull) | (held & 8u ? 0xffff0000ull : 0ull);
+                const uint64_t keep = lo | hi << 32;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    vf[mt] &= keep;
+            }
+        }
         const bool carry = carries(tg);
         if (carry)
             read_rows();
@@ -656,7 +752,8 @@ attn_partial_mfma(const AttnArgs a)
         float sc[4], mx = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            sc[i] = tg + static_cast<int32_t>(4 * g4) + i < end ? s[i] * qk_scale : -INFINITY;
+            sc[i] = tg + static_cast<int32_t>(4 * g4) + i < end && (!LISTED || (held >> i & 1u)) ? s[i] * qk_scale
+                                                                                                : -INFINITY;
             mx = fmaxf(mx, sc[i]);
         }
         mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -710,7 +807,7 @@ attn_partial_mfma(const AttnArgs a)
     __syncthreads();
     // the sequence's output if it is one partition, else a record; of the
     // group's query heads
-    const bool whole = parts == 1;
+    const bool whole = MODE != kAttnOwn && parts == 1;
     const uint32_t out_row = whole ? D : D + kAttnHeader, out_at = whole ? 0u : kAttnHeader;
     const uint64_t out_first = whole ? static_cast<uint64_t>(layer) * a.batch + b
                                      : static_cast<uint64_t>(layer) * a.n_records + item;
@@ -743,24 +840,36 @@ attn_partial_mfma(const AttnArgs a)
     }
 }
 
-template <int BF16, int D>
-const void *attn_kernel(bool migrating, bool units)
+template <int BF16, int D, int MODE>
+const void *attn_kernel(bool units)
 {
-    if (migrating)
-        return units ? reinterpret_cast<const void *>(&attn_partial_mfma<BF16, D, 1, 1>)
-                     : reinterpret_cast<const void *>(&attn_partial_mfma<BF16, D, 1, 0>);
-    return units ? reinterpret_cast<const void *>(&attn_partial_mfma<BF16, D, 0, 1>)
-                 : reinterpret_cast<const void *>(&attn_partial_mfma<BF16, D, 0, 0>);
+    return units ? reinterpret_cast<const void *>(&attn_partial_mfma<BF16, D, MODE, 1>)
+                 : reinterpret_cast<const void *>(&attn_partial_mfma<BF16, D, MODE, 0>);
 }
 
-const void *attn_kernel_for(int bf16, int head_dim, int group, bool migrating, bool units)
+template <int BF16, int D>
+const void *attn_kernel(AttnMode mode, bool units)
+{
+    switch (mode) {
+    case kAttnMigrating:
+        return attn_kernel<BF16, D, kAttnMigrating>(units);
+    case kAttnListed:
+        return attn_kernel<BF16, D, kAttnListed>(units);
+    case kAttnOwn:
+        return attn_kernel<BF16, D, kAttnOwn>(units);
+    default:
+        return attn_kernel<BF16, D, kAttnPlain>(units);
+    }
+}
+
+const void *attn_kernel_for(int bf16, int head_dim, int group, AttnMode mode, bool units)
 {
     if (group < 1 || group > 16 || (group & (group - 1)) != 0)
         return nullptr;
     if (head_dim == 64)
-        return bf16 ? attn_kernel<1, 64>(migrating, units) : attn_kernel<0, 64>(migrating, units);
+        return bf16 ? attn_kernel<1, 64>(mode, units) : attn_kernel<0, 64>(mode, units);
     if (head_dim == 128)
-        return bf16 ? attn_kernel<1, 128>(migrating, units) : attn_kernel<0, 128>(migrating, units);
+        return bf16 ? attn_kernel<1, 128>(mode, units) : attn_kernel<0, 128>(mode, units);
     return nullptr;
 }
 

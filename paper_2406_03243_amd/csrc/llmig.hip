@@ -8,7 +8,10 @@
 // helper), copy_tiles.h (the tile copy and its launch configuration),
 // convert_tiles.h (the copy between pools of different intra-tile
 // layouts), decode_attention.h (paged decode attention, the work measured
-// beside a migration), this file (pool registry, planner, coordinator,
+// beside a migration, also over listed blocks), prefix_attention.h (decode
+// attention behind a shared prefix), append_rotary.h (appends with the position
+// rotation), key_bounds.h (bounds of the blocks' keys and the choice of blocks
+// by them), this file (pool registry, planner, coordinator,
 // harness kernels, argument checks and the C ABI).
 
 #include <hip/hip_runtime.h>
@@ -22,6 +25,7 @@
 #include <memory>
 #include <mutex>
 #include <new>
+#include <type_traits>
 #include <utility>
 #include <vector>
 
@@ -30,6 +34,9 @@
 #include "convert_tiles.h"
 #include "copy_tiles.h"
 #include "decode_attention.h"
+#include "append_rotary.h"
+#include "key_bounds.h"
+#include "prefix_attention.h"
 
 struct llmig_pool {
     int32_t num_layers, num_blocks, block_size, num_kv_heads, head_dim, elem_bytes;
@@ -1086,6 +1093,8 @@ int llmig_stream_read(const void *region, int64_t bytes, int32_t passes, int32_t
     return e == hipSuccess ? LLMIG_OK : hip_error(e);
 }
 
+} // extern "C"
+
 // Work items of a decode-attention call: one per partition of kPartTokens
 // tokens of each sequence, in sequence order.  LLMIG_EINVAL for a negative
 // length.
@@ -1118,7 +1127,7 @@ static int attn_workspace_bytes(int64_t num_layers, int64_t n_items, int64_t q_h
 // on success gives the kernel, the item count and the workspace size.
 static int attn_check(const llmig_pool *pool, int32_t dtype, const void *q, int32_t batch, int32_t q_heads,
                       const int32_t *tables, int32_t table_stride, const int32_t *ctx_lens, const float *out,
-                      const void **fn, int64_t *n_items, int64_t *ws_bytes, bool migrating = false)
+                      const void **fn, int64_t *n_items, int64_t *ws_bytes, AttnMode mode = kAttnPlain)
 {
     if (!pool || !on_current_device(pool) || (dtype != 0 && dtype != 1) || pool->elem_bytes != 2 || !q ||
         !tables || !ctx_lens || !out || batch < 1 || batch > kAttnMaxBatch || q_heads < 1 || table_stride < 1 ||
@@ -1127,7 +1136,7 @@ static int attn_check(const llmig_pool *pool, int32_t dtype, const void *q, int3
     const int32_t hkv = pool->num_kv_heads;
     if (q_heads % hkv != 0)
         return LLMIG_EINVAL;
-    *fn = attn_kernel_for(dtype, pool->head_dim, q_heads / hkv, migrating, pool->block_size % 8 == 0);
+    *fn = attn_kernel_for(dtype, pool->head_dim, q_heads / hkv, mode, pool->block_size % 8 == 0);
     if (!*fn || (reinterpret_cast<uintptr_t>(q) & 15u) || (reinterpret_cast<uintptr_t>(out) & 15u) ||
         (reinterpret_cast<uintptr_t>(tables) & 3u))
         return LLMIG_EINVAL;
@@ -1149,17 +1158,18 @@ struct AttnMigration {
     const void *plain = nullptr;    // the kernel of a call that carries none
 };
 
-// Enqueues a checked decode-attention call: the partial kernel over the
-// items, then the merge of the sequences cut into several partitions.  ws
-// (ws_bytes, at least what partitions of kPartTokens need) holds the partial
-// results.  Allocates nothing.
-static int attn_enqueue(const llmig_pool *pool, const void *fn, const void *q, int32_t batch, int32_t q_heads,
-                        const int32_t *tables, int32_t table_stride, const int32_t *ctx_lens, float scale,
-                        float *ws, int64_t ws_bytes, float *out, hipStream_t st,
-                        const AttnMigration &mig = AttnMigration())
+// Launches the partial kernel `fn` of a checked call over partitions of at
+// most `part` tokens.  a (zeroed but for what its mode adds) is filled in, and
+// r with the sequences that leave records: those of several partitions, or
+// (all_records) every one; returns the most partitions of one of them.
+// Allocates nothing.
+template <class Args>
+static int attn_launch(Args &a, AttnReduceArgs &r, uint32_t *most_parts, const llmig_pool *pool, const void *fn,
+                       const void *q, int32_t batch, int32_t q_heads, const int32_t *tables, int32_t table_stride,
+                       const int32_t *ctx_lens, float scale, int32_t part, float *ws, float *out, hipStream_t st,
+                       const AttnMigration &mig, bool all_records)
 {
-    AttnArgs a;
-    std::memset(&a, 0, sizeof(a));
+    constexpr bool kListed = std::is_same<Args, AttnListedArgs>::value;
     a.mig_seq = -1;
     if (mig.dst) {
         a.dst_tab = mig.dst->d_tab;
@@ -1170,11 +1180,6 @@ static int attn_enqueue(const llmig_pool *pool, const void *fn, const void *q, i
         a.dst_layer_bytes = static_cast<uint32_t>(static_cast<uint64_t>(mig.dst->num_blocks) * mig.dst->tile_bytes);
         a.dst_blocks = mig.dst->num_blocks;
     }
-    int32_t part = attn_part_tokens(ctx_lens, batch, pool->num_layers, pool->num_kv_heads, pool->head_dim);
-    int64_t need = 0;
-    if (attn_record_bytes(ctx_lens, batch, part, pool->num_layers, q_heads, pool->head_dim, &need) != LLMIG_OK ||
-        need > ws_bytes)
-        part = kPartTokens;
     a.k_tab = pool->d_tab;
     a.q = static_cast<const uint8_t *>(q);
     a.tables = tables;
@@ -1210,7 +1215,6 @@ static int attn_enqueue(const llmig_pool *pool, const void *fn, const void *q, i
     if (apart)
         key[mig.seq] = static_cast<uint64_t>(mig.seq);
     std::sort(key, key + batch);
-    AttnReduceArgs r;
     std::memset(&r, 0, sizeof(r));
     uint32_t items = 0, most = 0;
     for (int32_t s = 0; s < batch; ++s) {
@@ -1221,7 +1225,7 @@ static int attn_enqueue(const llmig_pool *pool, const void *fn, const void *q, i
         a.ctx[s] = ctx_lens[b];
         const uint32_t len64 = parts > 1 ? static_cast<uint32_t>(attn_part_len(ctx_lens[b], parts) / 64) : 0u;
         a.seq[s / 2] |= (static_cast<uint32_t>(b) | len64 << 8) << (16 * (s % 2));
-        if (parts > 1) {
+        if (parts > 1 || all_records) {
             most = std::max(most, parts);
             r.seq_end[s] = items;
             r.seq[s] = static_cast<uint8_t>(b);
@@ -1231,7 +1235,7 @@ static int attn_enqueue(const llmig_pool *pool, const void *fn, const void *q, i
     }
     size_t lds = pool->block_size % 8 == 0
                      ? 0
-                     : attn_blk_slots(a.part_tokens, a.block_size) * sizeof(int32_t) * (mig.dst ? 2 : 1);
+                     : attn_blk_slots(a.part_tokens, a.block_size) * sizeof(int32_t) * (mig.dst || kListed ? 2 : 1);
     const int per_cu = attn_workgroups_per_cu(pool->head_dim, workgroups, tokens / n_items, mig.dst != nullptr);
     const bool by_layer = attn_layer_by_layer(pool->head_dim, workgroups, tokens / n_items);
     lds = std::max(lds, attn_spare_lds(pool->head_dim, per_cu));
@@ -1248,8 +1252,6 @@ static int attn_enqueue(const llmig_pool *pool, const void *fn, const void *q, i
             return hip_error(e);
         at += here;
     }
-    if (r.seqs == 0)
-        return LLMIG_OK;
     r.ws = ws;
     r.out = out;
     r.num_layers = a.num_layers;
@@ -1257,9 +1259,18 @@ static int attn_enqueue(const llmig_pool *pool, const void *fn, const void *q, i
     r.q_heads = a.q_heads;
     r.head_dim = static_cast<uint32_t>(pool->head_dim);
     r.n_records = a.n_records;
+    *most_parts = most;
+    return LLMIG_OK;
+}
+
+// The merge of the sequences cut into several partitions.
+static int attn_merge(AttnReduceArgs &r, uint32_t most, hipStream_t st)
+{
+    if (r.seqs == 0)
+        return LLMIG_OK;
     const uint64_t rows = static_cast<uint64_t>(r.num_layers) * r.seqs * r.q_heads;
     const void *rfn = nullptr;
-    const uint64_t per_wg = attn_reduce_kernel(pool->head_dim, most, &rfn);
+    const uint64_t per_wg = attn_reduce_kernel(static_cast<int>(r.head_dim), most, &rfn);
     for (r.row_base = 0; r.row_base < rows; r.row_base += kMaxGridWorkgroups * per_wg) {
         const uint64_t grid = (rows - r.row_base + per_wg - 1) / per_wg;
         void *rargs[] = {&r};
@@ -1270,6 +1281,31 @@ static int attn_enqueue(const llmig_pool *pool, const void *fn, const void *q, i
     }
     return LLMIG_OK;
 }
+
+// Enqueues a checked decode-attention call: the partial kernel over the
+// items, then the merge of the sequences cut into several partitions.  ws
+// (ws_bytes, at least what partitions of kPartTokens need) holds the partial
+// results.  Allocates nothing.
+static int attn_enqueue(const llmig_pool *pool, const void *fn, const void *q, int32_t batch, int32_t q_heads,
+                        const int32_t *tables, int32_t table_stride, const int32_t *ctx_lens, float scale,
+                        float *ws, int64_t ws_bytes, float *out, hipStream_t st,
+                        const AttnMigration &mig = AttnMigration())
+{
+    AttnArgs a;
+    std::memset(&a, 0, sizeof(a));
+    int32_t part = attn_part_tokens(ctx_lens, batch, pool->num_layers, pool->num_kv_heads, pool->head_dim);
+    int64_t need = 0;
+    if (attn_record_bytes(ctx_lens, batch, part, pool->num_layers, q_heads, pool->head_dim, &need) != LLMIG_OK ||
+        need > ws_bytes)
+        part = kPartTokens;
+    AttnReduceArgs r;
+    uint32_t most = 0;
+    const int rc = attn_launch(a, r, &most, pool, fn, q, batch, q_heads, tables, table_stride, ctx_lens, scale, part,
+                               ws, out, st, mig, false);
+    return rc == LLMIG_OK ? attn_merge(r, most, st) : rc;
+}
+
+extern "C" {
 
 int llmig_decode_attention_workspace(const int32_t *ctx_lens, int32_t batch, int32_t num_layers, int32_t q_heads,
                                      int32_t head_dim, int64_t *bytes)
@@ -1325,7 +1361,7 @@ int llmig_decode_attention_migrate(const llmig_pool *pool, int32_t dtype, const 
     const void *fn = nullptr;
     int64_t n_items = 0, need = 0;
     int rc = attn_check(pool, dtype, q, batch, q_heads, tables, table_stride, ctx_lens, out, &fn, &n_items, &need,
-                        true);
+                        kAttnMigrating);
     if (rc != LLMIG_OK)
         return rc;
     if ((reinterpret_cast<uintptr_t>(workspace) & 15u) || !workspace || workspace_bytes < need)
@@ -1344,7 +1380,7 @@ int llmig_decode_attention_migrate(const llmig_pool *pool, int32_t dtype, const 
     mig.ids = dst_ids;
     mig.from = static_cast<int32_t>(from_block);
     mig.to = static_cast<int32_t>(to_block);
-    mig.plain = attn_kernel_for(dtype, pool->head_dim, q_heads / pool->num_kv_heads, false, pool->block_size % 8 == 0);
+    mig.plain = attn_kernel_for(dtype, pool->head_dim, q_heads / pool->num_kv_heads, kAttnPlain, pool->block_size % 8 == 0);
     return attn_enqueue(pool, fn, q, batch, q_heads, tables, table_stride, ctx_lens, scale,
                         static_cast<float *>(workspace), workspace_bytes, out, static_cast<hipStream_t>(stream), mig);
 }
@@ -1369,6 +1405,484 @@ int llmig_decode_attention_noalloc(const llmig_pool *pool, int32_t dtype, const 
         return attn_enqueue(pool, fn, q, batch, q_heads, tables, table_stride, ctx_lens, scale,
                             static_cast<float *>(ws), LLMIG_DECODE_SCRATCH_BYTES, out, static_cast<hipStream_t>(stream));
     });
+}
+
+} // extern "C"
+
+// Launches `fn` on items 0 .. items - 1 of a call, one workgroup an item, in
+// launches that the grid can hold; `first` is set to a launch's first item, in
+// units of `per` items.
+static int launch_items(const void *fn, void *args, uint64_t items, uint32_t per, uint32_t *first, hipStream_t st)
+{
+    const uint64_t step = std::max<uint64_t>(kMaxGridWorkgroups / per, 1) * per;
+    for (uint64_t at = 0; at < items; at += step) {
+        *first = static_cast<uint32_t>(at / per);
+        void *list[] = {args};
+        const hipError_t e = hipLaunchKernel(fn, dim3(static_cast<uint32_t>(std::min(step, items - at))), dim3(kThreads),
+                                             list, 0, st);
+        if (e != hipSuccess)
+            return hip_error(e);
+    }
+    return LLMIG_OK;
+}
+
+// The bytes [begin, end) that rows of an array touch.
+static std::pair<uint64_t, uint64_t> row_span(const void *p, int64_t layers, int64_t layer, int64_t rows, int64_t row,
+                                              int64_t elements)
+{
+    const uint64_t b = reinterpret_cast<uint64_t>(p);
+    return {b, b + 2u * static_cast<uint64_t>((layers - 1) * layer + (rows - 1) * row + elements)};
+}
+
+// Whether a pool's bounds are kept in `bounds` (llmig_key_bounds).
+static bool bounds_pool(const llmig_pool *bounds)
+{
+    return bounds->block_size == 1 && bounds->elem_bytes == 2 && bounds->head_dim % 8 == 0 &&
+           bounds->layouts[0] == LLMIG_LAYOUT_NHD && bounds->layouts[1] == LLMIG_LAYOUT_NHD &&
+           on_current_device(bounds);
+}
+
+static int32_t blocks_of(int32_t tokens, int32_t block_size)
+{
+    return tokens / block_size + (tokens % block_size != 0);
+}
+
+// Partial results of attention over listed blocks: the virtual lengths, how
+// they are cut, and the bytes of the records.
+static int listed_cut(const llmig_pool *pool, const int32_t *ctx_lens, int32_t batch, int32_t q_heads, int32_t count,
+                      int32_t *lens, int32_t *part, int64_t *bytes)
+{
+    if (count < 1)
+        return LLMIG_EINVAL;
+    for (int32_t b = 0; b < batch; ++b) {
+        if (ctx_lens[b] < 0)
+            return LLMIG_EINVAL;
+        const int64_t n = static_cast<int64_t>(std::min(count, blocks_of(ctx_lens[b], pool->block_size))) * pool->block_size;
+        if (n > 0x7fffffffLL - 64)
+            return LLMIG_EINVAL;
+        lens[b] = static_cast<int32_t>(n);
+    }
+    *part = attn_part_tokens(lens, batch, pool->num_layers, pool->num_kv_heads, pool->head_dim);
+    return attn_record_bytes(lens, batch, *part, pool->num_layers, q_heads, pool->head_dim, bytes);
+}
+
+// How a call behind a shared prefix is cut.  members 0: not at all, the call is
+// plain decode attention.
+struct PrefixPlan {
+    uint32_t members;
+    PrefixCut cut;
+    int32_t part;                       // of the own tokens
+    int32_t own[kAttnMaxBatch];         // tokens that a sequence's own items cover
+    uint8_t member[kAttnMaxBatch];      // sequences behind the prefix
+    int64_t prefix_bytes, own_bytes;    // of the records
+};
+
+static int prefix_plan(const llmig_pool *pool, const int32_t *ctx_lens, int32_t batch, int32_t q_heads,
+                       int32_t prefix_blocks, PrefixPlan *p)
+{
+    std::memset(p, 0, sizeof(*p));
+    const int64_t tokens = static_cast<int64_t>(prefix_blocks) * pool->block_size;
+    const int64_t L = pool->num_layers, H = pool->num_kv_heads, D = pool->head_dim;
+    for (int32_t b = 0; b < batch; ++b) {
+        if (ctx_lens[b] < 0)
+            return LLMIG_EINVAL;
+        if (tokens > 0 && ctx_lens[b] >= tokens)
+            p->member[p->members++] = static_cast<uint8_t>(b);
+    }
+    if (p->members < 2)
+        p->members = 0;
+    for (int32_t b = 0; b < batch; ++b)
+        p->own[b] = p->members && ctx_lens[b] >= tokens ? static_cast<int32_t>(ctx_lens[b] - tokens) : ctx_lens[b];
+    p->part = attn_part_tokens(p->own, batch, L, H, D);
+    if (!p->members)
+        return attn_record_bytes(p->own, batch, p->part, L, q_heads, D, &p->own_bytes);
+    p->cut = prefix_cut(p->members * static_cast<uint32_t>(q_heads / H), tokens, L * H);
+    int64_t v = 0;
+    if (__builtin_mul_overflow(attn_items(p->own, batch, p->part), L * q_heads, &v) ||
+        __builtin_mul_overflow(v, (D + kAttnHeader) * 4, &p->own_bytes) ||
+        __builtin_mul_overflow(static_cast<int64_t>(p->cut.parts) * p->members, L * q_heads, &v) ||
+        __builtin_mul_overflow(v, (D + kAttnHeader) * 4, &p->prefix_bytes) ||
+        p->prefix_bytes > INT64_MAX - p->own_bytes)
+        return LLMIG_EINVAL;
+    return LLMIG_OK;
+}
+
+extern "C" {
+
+int llmig_append_rotary(const llmig_pool *pool, const llmig_append_desc *d, void *stream)
+{
+    if (!pool || !d || !on_current_device(pool) || (d->dtype != 0 && d->dtype != 1) || pool->elem_bytes != 2 ||
+        pool->head_dim % 8 != 0 || d->batch < 1 || d->batch > kAppendMaxBatch || d->q_heads < 0 || d->table_stride < 1 ||
+        !d->tables || !d->from_toks || !d->n_toks || (d->interleaved != 0 && d->interleaved != 1) || d->rotary_dim < 0 ||
+        d->rotary_dim % 2 != 0 || d->rotary_dim > pool->head_dim || (reinterpret_cast<uintptr_t>(d->tables) & 3u))
+        return LLMIG_EINVAL;
+    if (d->rotary_dim > 0 && (!d->cos_sin || (reinterpret_cast<uintptr_t>(d->cos_sin) & 3u) || d->positions < 1))
+        return LLMIG_EINVAL;
+    const int64_t L = pool->num_layers, bs = pool->block_size, D = pool->head_dim;
+    AppendArgs a;
+    std::memset(&a, 0, sizeof(a));
+    int64_t n = 0;
+    for (int32_t b = 0; b < d->batch; ++b) {
+        const int64_t from = d->from_toks[b], add = d->n_toks[b], pos = d->first_pos ? d->first_pos[b] : from;
+        if (from < 0 || add < 0 || pos < 0 || from + add > 0x7fffffffLL)
+            return LLMIG_EINVAL;
+        if (add > 0 && ((from + add - 1) / bs >= d->table_stride || (d->rotary_dim > 0 && pos + add > d->positions)))
+            return LLMIG_EINVAL;
+        n += add;
+        if (n > 0x7fffffffLL / L)
+            return LLMIG_EINVAL;
+        a.token_end[b] = static_cast<uint32_t>(n);
+        a.from[b] = d->from_toks[b];
+        a.pos[b] = static_cast<int32_t>(pos);
+    }
+    if (n == 0)
+        return LLMIG_OK;
+    const void *x[3] = {d->q, d->k, d->v};
+    const int64_t layer[3] = {d->q_layer, d->k_layer, d->v_layer}, token[3] = {d->q_token, d->k_token, d->v_token};
+    const int64_t row[3] = {d->q_heads * D, pool->num_kv_heads * D, pool->num_kv_heads * D};
+    // rows of a call that 32-bit chunk numbers cannot count are refused
+    if (d->q_heads + 2ll * pool->num_kv_heads > (1 << 24) / (D / 8))
+        return LLMIG_EINVAL;
+    for (int k = d->q_heads > 0 ? 0 : 1; k < 3; ++k) {
+        if (!x[k] || (reinterpret_cast<uintptr_t>(x[k]) & 15u) || layer[k] < 0 || token[k] < 0 || layer[k] % 8 != 0 ||
+            token[k] % 8 != 0 || layer[k] > (INT64_MAX / 8) / L || token[k] > (INT64_MAX / 8) / n)
+            return LLMIG_EINVAL;
+        a.x[k] = static_cast<const uint8_t *>(x[k]);
+        a.layer_bytes[k] = static_cast<uint64_t>(layer[k]) * 2u;
+        a.token_bytes[k] = static_cast<uint64_t>(token[k]) * 2u;
+    }
+    if (d->q_heads > 0) {
+        if (!d->q_out || (reinterpret_cast<uintptr_t>(d->q_out) & 15u))
+            return LLMIG_EINVAL;
+        const auto out = row_span(d->q_out, L, n * row[0], n, row[0], row[0]);
+        for (int k = 0; k < 3; ++k) {
+            const auto in = row_span(x[k], L, layer[k], n, token[k], row[k]);
+            if (in.first < out.second && out.first < in.second)
+                return LLMIG_EINVAL;
+        }
+    }
+    a.tab = pool->d_tab;
+    a.q_out = static_cast<uint8_t *>(d->q_out);
+    a.tables = d->tables;
+    a.cos_sin = d->cos_sin;
+    a.num_layers = static_cast<uint32_t>(L);
+    a.num_blocks = static_cast<uint32_t>(pool->num_blocks);
+    a.block_size = static_cast<uint32_t>(bs);
+    a.table_stride = static_cast<uint32_t>(d->table_stride);
+    a.tile_bytes = static_cast<uint32_t>(pool->tile_bytes);
+    a.q_heads = static_cast<uint32_t>(d->q_heads);
+    a.kv_heads = static_cast<uint32_t>(pool->num_kv_heads);
+    a.tokens = static_cast<uint32_t>(n);
+    a.batch = static_cast<uint32_t>(d->batch);
+    a.row_chunks = static_cast<uint32_t>(D / 8);
+    a.token_chunks = (a.q_heads + 2u * a.kv_heads) * a.row_chunks;
+    a.half = static_cast<uint32_t>(d->rotary_dim / 2);
+    a.interleaved = static_cast<uint32_t>(d->interleaved);
+    a.wide = a.half % 4 == 0 && (reinterpret_cast<uintptr_t>(d->cos_sin) & 15u) == 0;
+    a.layouts[0] = pool->layouts[0];
+    a.layouts[1] = pool->layouts[1];
+    const uint32_t slices = (a.token_chunks + kThreads - 1) / kThreads;
+    a.by_slice = divisor(slices);
+    a.by_layer = divisor(a.num_layers);
+    a.by_row = divisor(a.row_chunks);
+    a.by_block = divisor(a.block_size);
+    const void *fn = d->dtype ? reinterpret_cast<const void *>(&append_rotary_rows<1>)
+                              : reinterpret_cast<const void *>(&append_rotary_rows<0>);
+    return launch_items(fn, &a, static_cast<uint64_t>(n) * L * slices, slices, &a.first_unit,
+                        static_cast<hipStream_t>(stream));
+}
+
+int llmig_key_bounds(const llmig_pool *pool, const llmig_pool *bounds, int32_t dtype, int32_t batch,
+                     const int32_t *tables, int32_t table_stride, const int32_t *from_toks, const int32_t *ctx_lens,
+                     void *stream)
+{
+    if (!pool || !bounds || !on_current_device(pool) || (dtype != 0 && dtype != 1) || pool->elem_bytes != 2 ||
+        pool->layouts[0] != LLMIG_LAYOUT_NHD || pool->layouts[1] != LLMIG_LAYOUT_NHD || !bounds_pool(bounds) ||
+        pool->num_layers != bounds->num_layers || pool->num_blocks != bounds->num_blocks ||
+        pool->num_kv_heads != bounds->num_kv_heads || pool->head_dim != bounds->head_dim || pools_overlap(pool, bounds) ||
+        batch < 1 || batch > kAppendMaxBatch || !tables || (reinterpret_cast<uintptr_t>(tables) & 3u) ||
+        table_stride < 1 || !from_toks || !ctx_lens)
+        return LLMIG_EINVAL;
+    BoundsArgs a;
+    std::memset(&a, 0, sizeof(a));
+    int64_t n = 0;
+    for (int32_t b = 0; b < batch; ++b) {
+        if (from_toks[b] < 0 || from_toks[b] > ctx_lens[b] || blocks_of(ctx_lens[b], pool->block_size) > table_stride)
+            return LLMIG_EINVAL;
+        a.first_block[b] = from_toks[b] / pool->block_size;
+        a.tokens[b] = ctx_lens[b];
+        if (from_toks[b] < ctx_lens[b])
+            n += blocks_of(ctx_lens[b], pool->block_size) - a.first_block[b];
+        a.block_end[b] = static_cast<uint32_t>(n);
+    }
+    a.slot_chunks = static_cast<uint32_t>(pool->num_kv_heads * (pool->head_dim / 8));
+    const uint32_t slices = (a.slot_chunks + kThreads - 1) / kThreads;
+    if (n > 0x7fffffffLL / pool->num_layers / slices)
+        return LLMIG_EINVAL;
+    if (n == 0)
+        return LLMIG_OK;
+    a.tab = pool->d_tab;
+    a.bounds_tab = bounds->d_tab;
+    a.tables = tables;
+    a.num_layers = static_cast<uint32_t>(pool->num_layers);
+    a.num_blocks = static_cast<uint32_t>(pool->num_blocks);
+    a.block_size = static_cast<uint32_t>(pool->block_size);
+    a.table_stride = static_cast<uint32_t>(table_stride);
+    a.tile_bytes = static_cast<uint32_t>(pool->tile_bytes);
+    a.batch = static_cast<uint32_t>(batch);
+    a.blocks = static_cast<uint32_t>(n);
+    a.by_slice = divisor(slices);
+    a.by_block = divisor(a.blocks);
+    const void *fn = dtype ? reinterpret_cast<const void *>(&key_bounds_rows<1>)
+                           : reinterpret_cast<const void *>(&key_bounds_rows<0>);
+    return launch_items(fn, &a, static_cast<uint64_t>(n) * pool->num_layers * slices, 1, &a.first_item,
+                        static_cast<hipStream_t>(stream));
+}
+
+int llmig_select_blocks_workspace(const llmig_pool *bounds, int32_t block_size, const int32_t *ctx_lens,
+                                  int32_t batch, int64_t *bytes)
+{
+    if (!bytes)
+        return LLMIG_EINVAL;
+    *bytes = 0;
+    if (!bounds || block_size < 1 || !ctx_lens || batch < 1 || batch > kAppendMaxBatch)
+        return LLMIG_EINVAL;
+    int64_t n = 0;
+    for (int32_t b = 0; b < batch; ++b) {
+        if (ctx_lens[b] < 0)
+            return LLMIG_EINVAL;
+        n += blocks_of(ctx_lens[b], block_size);
+    }
+    int64_t v = 0;
+    if (__builtin_mul_overflow(n * 8, static_cast<int64_t>(bounds->num_layers) * bounds->num_kv_heads, &v))
+        return LLMIG_EINVAL;
+    *bytes = v;
+    return LLMIG_OK;
+}
+
+int llmig_select_blocks(const llmig_pool *bounds, int32_t dtype, int32_t block_size, const void *q, int32_t batch,
+                        int32_t q_heads, const int32_t *tables, int32_t table_stride, const int32_t *ctx_lens,
+                        int32_t keep_first, int32_t keep_last, int32_t count, void *workspace, int64_t workspace_bytes,
+                        int32_t *blocks, void *stream)
+{
+    int64_t need = 0;
+    if (!bounds || !bounds_pool(bounds) || (bounds->head_dim != 64 && bounds->head_dim != 128) ||
+        (dtype != 0 && dtype != 1) || !q || (reinterpret_cast<uintptr_t>(q) & 15u) || !tables ||
+        (reinterpret_cast<uintptr_t>(tables) & 3u) || table_stride < 1 || !blocks ||
+        (reinterpret_cast<uintptr_t>(blocks) & 3u) || q_heads < 1 || q_heads % bounds->num_kv_heads != 0 ||
+        keep_first < 0 || keep_last < 0 || count < 1 || static_cast<int64_t>(keep_first) + keep_last > count ||
+        llmig_select_blocks_workspace(bounds, block_size, ctx_lens, batch, &need) != LLMIG_OK)
+        return LLMIG_EINVAL;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 7u) || (need > 0 && (!workspace || workspace_bytes < need)))
+        return LLMIG_EINVAL;
+    SelectArgs a;
+    std::memset(&a, 0, sizeof(a));
+    int64_t n = 0;
+    uint32_t longest = 0;
+    for (int32_t b = 0; b < batch; ++b) {
+        const int32_t here = blocks_of(ctx_lens[b], block_size);
+        if (here > table_stride)
+            return LLMIG_EINVAL;
+        n += here;
+        a.block_end[b] = static_cast<uint32_t>(n);
+        longest = std::max(longest, static_cast<uint32_t>(here));
+    }
+    const uint32_t row = static_cast<uint32_t>(bounds->num_kv_heads * (bounds->head_dim / 8));
+    const uint32_t rows = row < kThreads ? kThreads / row : 1u;
+    a.tab = bounds->d_tab;
+    a.q = static_cast<const uint8_t *>(q);
+    a.tables = tables;
+    a.keys = static_cast<uint64_t *>(workspace);
+    a.out = blocks;
+    a.num_layers = static_cast<uint32_t>(bounds->num_layers);
+    a.num_blocks = static_cast<uint32_t>(bounds->num_blocks);
+    a.batch = static_cast<uint32_t>(batch);
+    a.q_heads = static_cast<uint32_t>(q_heads);
+    a.kv_heads = static_cast<uint32_t>(bounds->num_kv_heads);
+    a.table_stride = static_cast<uint32_t>(table_stride);
+    a.keep_first = static_cast<uint32_t>(keep_first);
+    a.keep_last = static_cast<uint32_t>(keep_last);
+    a.count = static_cast<uint32_t>(count);
+    a.blocks = static_cast<uint32_t>(n);
+    a.parts = std::max(1u, (longest + rows * kScoreBlocks - 1) / (rows * kScoreBlocks));
+    a.slices = (row + kThreads - 1) / kThreads;
+    const uint64_t lists = static_cast<uint64_t>(a.num_layers) * a.batch * a.kv_heads;
+    const uint64_t items = static_cast<uint64_t>(a.num_layers) * a.batch * a.slices * a.parts;
+    if (n > 0x7fffffffLL || items > 0x7fffffffull || lists > 0x7fffffffull)
+        return LLMIG_EINVAL;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (longest > a.count) {
+        const void *fn = bounds->head_dim == 64
+                             ? dtype ? reinterpret_cast<const void *>(&score_blocks<1, 64>)
+                                     : reinterpret_cast<const void *>(&score_blocks<0, 64>)
+                         : dtype ? reinterpret_cast<const void *>(&score_blocks<1, 128>)
+                                 : reinterpret_cast<const void *>(&score_blocks<0, 128>);
+        const int rc = launch_items(fn, &a, items, 1, &a.first_item, st);
+        if (rc != LLMIG_OK)
+            return rc;
+    }
+    return launch_items(reinterpret_cast<const void *>(&list_blocks), &a, lists, 1, &a.first_item, st);
+}
+
+int llmig_decode_attention_blocks_workspace(const llmig_pool *pool, const int32_t *ctx_lens, int32_t batch,
+                                            int32_t q_heads, int32_t count, int64_t *bytes)
+{
+    if (!bytes)
+        return LLMIG_EINVAL;
+    *bytes = 0;
+    if (!pool || !ctx_lens || batch < 1 || batch > kAttnMaxBatch || q_heads < 1)
+        return LLMIG_EINVAL;
+    int32_t lens[kAttnMaxBatch], part = 0;
+    return listed_cut(pool, ctx_lens, batch, q_heads, count, lens, &part, bytes);
+}
+
+int llmig_decode_attention_blocks(const llmig_pool *pool, int32_t dtype, const void *q, int32_t batch, int32_t q_heads,
+                                  const int32_t *tables, int32_t table_stride, const int32_t *ctx_lens,
+                                  const int32_t *blocks, int32_t count, float scale, void *workspace,
+                                  int64_t workspace_bytes, float *out, void *stream)
+{
+    const void *fn = nullptr;
+    int64_t n_items = 0, need = 0;
+    int rc = attn_check(pool, dtype, q, batch, q_heads, tables, table_stride, ctx_lens, out, &fn, &n_items, &need,
+                        kAttnListed);
+    if (rc != LLMIG_OK)
+        return rc;
+    int32_t lens[kAttnMaxBatch], part = 0;
+    rc = listed_cut(pool, ctx_lens, batch, q_heads, count, lens, &part, &need);
+    if (rc != LLMIG_OK)
+        return rc;
+    if (!blocks || (reinterpret_cast<uintptr_t>(blocks) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 15u) ||
+        (need > 0 && (!workspace || workspace_bytes < need)))
+        return LLMIG_EINVAL;
+    AttnListedArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.lists = blocks;
+    a.count = static_cast<uint32_t>(count);
+    a.num_blocks = static_cast<uint32_t>(pool->num_blocks);
+    std::memcpy(a.tokens, ctx_lens, static_cast<size_t>(batch) * sizeof(int32_t));
+    AttnReduceArgs r;
+    uint32_t most = 0;
+    rc = attn_launch(a, r, &most, pool, fn, q, batch, q_heads, tables, table_stride, lens, scale, part,
+                     static_cast<float *>(workspace), out, static_cast<hipStream_t>(stream), AttnMigration(), false);
+    return rc == LLMIG_OK ? attn_merge(r, most, static_cast<hipStream_t>(stream)) : rc;
+}
+
+int llmig_decode_attention_prefix_workspace(const llmig_pool *pool, const int32_t *ctx_lens, int32_t batch,
+                                            int32_t q_heads, int32_t prefix_blocks, int64_t *bytes)
+{
+    if (!bytes)
+        return LLMIG_EINVAL;
+    *bytes = 0;
+    if (!pool || !ctx_lens || batch < 1 || batch > kAttnMaxBatch || q_heads < 1 || q_heads % pool->num_kv_heads != 0 ||
+        prefix_blocks < 0)
+        return LLMIG_EINVAL;
+    PrefixPlan p;
+    const int rc = prefix_plan(pool, ctx_lens, batch, q_heads, prefix_blocks, &p);
+    if (rc == LLMIG_OK)
+        *bytes = p.prefix_bytes + p.own_bytes;
+    return rc;
+}
+
+int llmig_decode_attention_prefix(const llmig_pool *pool, int32_t dtype, const void *q, int32_t batch, int32_t q_heads,
+                                  const int32_t *tables, int32_t table_stride, const int32_t *ctx_lens,
+                                  int32_t prefix_blocks, float scale, void *workspace, int64_t workspace_bytes,
+                                  float *out, void *stream)
+{
+    const void *fn = nullptr;
+    int64_t n_items = 0, need = 0;
+    int rc = attn_check(pool, dtype, q, batch, q_heads, tables, table_stride, ctx_lens, out, &fn, &n_items, &need,
+                        kAttnOwn);
+    if (rc != LLMIG_OK)
+        return rc;
+    if (prefix_blocks < 0 || prefix_blocks > table_stride)
+        return LLMIG_EINVAL;
+    PrefixPlan p;
+    rc = prefix_plan(pool, ctx_lens, batch, q_heads, prefix_blocks, &p);
+    if (rc != LLMIG_OK)
+        return rc;
+    need = p.prefix_bytes + p.own_bytes;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 15u) || (need > 0 && (!workspace || workspace_bytes < need)))
+        return LLMIG_EINVAL;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (!p.members)
+        return attn_enqueue(pool, attn_kernel_for(dtype, pool->head_dim, q_heads / pool->num_kv_heads, kAttnPlain,
+                                                  pool->block_size % 8 == 0),
+                            q, batch, q_heads, tables, table_stride, ctx_lens, scale, static_cast<float *>(workspace),
+                            workspace_bytes, out, st);
+    const uint64_t rows = static_cast<uint64_t>(pool->num_layers) * batch * q_heads;
+    const uint64_t grid = static_cast<uint64_t>(pool->num_layers) * p.cut.parts * pool->num_kv_heads * p.cut.chunks;
+    if (rows > 0x7fffffffull || grid > kMaxGridWorkgroups)
+        return LLMIG_EINVAL;
+    PrefixArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.tab = pool->d_tab;
+    a.q = static_cast<const uint8_t *>(q);
+    a.table = tables + static_cast<int64_t>(p.member[0]) * table_stride;
+    a.ws = static_cast<float *>(workspace);
+    a.scale = scale;
+    a.num_layers = static_cast<uint32_t>(pool->num_layers);
+    a.batch = static_cast<uint32_t>(batch);
+    a.q_heads = static_cast<uint32_t>(q_heads);
+    a.kv_heads = static_cast<uint32_t>(pool->num_kv_heads);
+    a.num_blocks = static_cast<uint32_t>(pool->num_blocks);
+    a.block_size = static_cast<uint32_t>(pool->block_size);
+    a.tokens = static_cast<uint32_t>(prefix_blocks) * a.block_size;
+    a.part_tokens = p.cut.part_tokens;
+    a.parts = p.cut.parts;
+    a.members = p.members;
+    a.chunks = p.cut.chunks;
+    a.by_block = divisor(a.block_size);
+    std::memcpy(a.member, p.member, sizeof(a.member));
+    void *args[] = {&a};
+    hipError_t e = hipLaunchKernel(prefix_kernel_for(dtype, pool->head_dim, p.cut.wm), dim3(static_cast<uint32_t>(grid)),
+                                   dim3(kThreads), args, 0, st);
+    if (e != hipSuccess)
+        return hip_error(e);
+    AttnOwnArgs o;
+    std::memset(&o, 0, sizeof(o));
+    o.skip = static_cast<uint32_t>(prefix_blocks);
+    PrefixJoinArgs j;
+    std::memset(&j, 0, sizeof(j));
+    uint16_t place[kAttnMaxBatch];
+    for (int32_t b = 0; b < batch; ++b)
+        place[b] = static_cast<uint16_t>(p.members);
+    for (uint32_t k = 0; k < p.members; ++k) {
+        o.behind[p.member[k] / 32] |= 1u << (p.member[k] % 32);
+        place[p.member[k]] = static_cast<uint16_t>(k);
+    }
+    AttnReduceArgs r;
+    uint32_t most = 0;
+    float *own = static_cast<float *>(workspace) + p.prefix_bytes / 4;
+    rc = attn_launch(o, r, &most, pool, fn, q, batch, q_heads, tables, table_stride, p.own, scale, p.part, own, out, st,
+                     AttnMigration(), true);
+    if (rc != LLMIG_OK)
+        return rc;
+    j.prefix = static_cast<const float *>(workspace);
+    j.own = own;
+    j.out = out;
+    j.num_layers = a.num_layers;
+    j.batch = a.batch;
+    j.q_heads = a.q_heads;
+    j.parts = a.parts;
+    j.members = a.members;
+    j.n_records = r.n_records;
+    for (int32_t s = 0; s < batch; ++s) {
+        j.seq_end[s] = r.seq_end[s];
+        j.seq[s] = r.seq[s];
+        j.member[s] = place[r.seq[s]];
+    }
+    const void *jfn = pool->head_dim == 64 ? reinterpret_cast<const void *>(&prefix_join<64>)
+                                           : reinterpret_cast<const void *>(&prefix_join<128>);
+    const uint64_t per = kThreads / (pool->head_dim / 4);
+    for (uint64_t at = 0; at < rows; at += kMaxGridWorkgroups * per) {
+        j.row_base = static_cast<uint32_t>(at);
+        void *jargs[] = {&j};
+        e = hipLaunchKernel(jfn, dim3(static_cast<uint32_t>(std::min<uint64_t>((rows - at + per - 1) / per, kMaxGridWorkgroups))),
+                            dim3(kThreads), jargs, 0, st);
+        if (e != hipSuccess)
+            return hip_error(e);
+    }
+    return LLMIG_OK;
 }
 
 const char *llmig_strerror(int code)

@@ -113,6 +113,39 @@ _lib.llmig_decode_attention_migrate.restype = ctypes.c_int
 _lib.llmig_decode_attention_noalloc.argtypes = [_vp, ctypes.c_int32, _vp, ctypes.c_int32, ctypes.c_int32, _vp,
                                                 ctypes.c_int32, _vp, ctypes.c_float, _vp, _vp]
 _lib.llmig_decode_attention_noalloc.restype = ctypes.c_int
+
+
+class _AppendDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("q_heads", ctypes.c_int32),
+                ("table_stride", ctypes.c_int32), ("q", _vp), ("k", _vp), ("v", _vp), ("q_out", _vp),
+                ("q_layer", ctypes.c_int64), ("q_token", ctypes.c_int64), ("k_layer", ctypes.c_int64),
+                ("k_token", ctypes.c_int64), ("v_layer", ctypes.c_int64), ("v_token", ctypes.c_int64),
+                ("tables", _vp), ("from_toks", _vp), ("n_toks", _vp), ("first_pos", _vp), ("cos_sin", _vp),
+                ("positions", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+_lib.llmig_append_rotary.argtypes = [_vp, ctypes.POINTER(_AppendDesc), _vp]
+_lib.llmig_append_rotary.restype = ctypes.c_int
+_lib.llmig_key_bounds.argtypes = [_vp, _vp, ctypes.c_int32, ctypes.c_int32, _vp, ctypes.c_int32, _vp, _vp, _vp]
+_lib.llmig_key_bounds.restype = ctypes.c_int
+_lib.llmig_select_blocks_workspace.argtypes = [_vp, ctypes.c_int32, _vp, ctypes.c_int32, _i64p]
+_lib.llmig_select_blocks_workspace.restype = ctypes.c_int
+_lib.llmig_select_blocks.argtypes = [_vp, ctypes.c_int32, ctypes.c_int32, _vp, ctypes.c_int32, ctypes.c_int32, _vp,
+                                     ctypes.c_int32, _vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp,
+                                     ctypes.c_int64, _vp, _vp]
+_lib.llmig_select_blocks.restype = ctypes.c_int
+_lib.llmig_decode_attention_blocks_workspace.argtypes = [_vp, _vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _i64p]
+_lib.llmig_decode_attention_blocks_workspace.restype = ctypes.c_int
+_lib.llmig_decode_attention_blocks.argtypes = [_vp, ctypes.c_int32, _vp, ctypes.c_int32, ctypes.c_int32, _vp,
+                                               ctypes.c_int32, _vp, _vp, ctypes.c_int32, ctypes.c_float, _vp,
+                                               ctypes.c_int64, _vp, _vp]
+_lib.llmig_decode_attention_blocks.restype = ctypes.c_int
+_lib.llmig_decode_attention_prefix_workspace.argtypes = [_vp, _vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _i64p]
+_lib.llmig_decode_attention_prefix_workspace.restype = ctypes.c_int
+_lib.llmig_decode_attention_prefix.argtypes = [_vp, ctypes.c_int32, _vp, ctypes.c_int32, ctypes.c_int32, _vp,
+                                               ctypes.c_int32, _vp, ctypes.c_int32, ctypes.c_float, _vp, ctypes.c_int64,
+                                               _vp, _vp]
+_lib.llmig_decode_attention_prefix.restype = ctypes.c_int
 _lib.llmig_strerror.argtypes = [ctypes.c_int]
 _lib.llmig_strerror.restype = ctypes.c_char_p
 _lib.llmig_last_hip_error.argtypes = []
@@ -502,3 +535,176 @@ def llmig_decode_attention_noalloc(pool: Pool, q: torch.Tensor, tables: torch.Te
                                                c.ctypes.data, float(scale), out.data_ptr(), _stream(stream)),
            "llmig_decode_attention_noalloc")
     _used_on(stream, q, tables, out)
+
+
+def _dtype_code(t: torch.Tensor, what: str) -> int:
+    if t.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError(f"{what} must be fp16 or bf16")
+    return 1 if t.dtype == torch.bfloat16 else 0
+
+
+def _device_tables(tables: torch.Tensor, batch: int) -> None:
+    if tables.dtype != torch.int32 or not tables.is_cuda or not tables.is_contiguous() or tables.dim() != 2:
+        raise ValueError("tables must be a contiguous CUDA int32 [batch][stride] tensor")
+    if tables.shape[0] < batch:
+        raise ValueError("tables must hold a row per sequence")
+
+
+def _workspace(workspace: torch.Tensor) -> int:
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor")
+    return workspace.numel() * workspace.element_size()
+
+
+def _row_strides(t: torch.Tensor | None):
+    """Layer and token strides; 0 along an axis of one entry, whose stride in
+    torch may be any number."""
+    if t is None:
+        return 0, 0
+    return tuple(t.stride(i) if t.shape[i] > 1 else 0 for i in (0, 1))
+
+
+def llmig_append_rotary(pool: Pool, k: torch.Tensor, v: torch.Tensor, tables: torch.Tensor, from_toks, n_toks,
+                        cos_sin: torch.Tensor | None, q: torch.Tensor | None = None,
+                        q_out: torch.Tensor | None = None, interleaved: bool = False, first_pos=None,
+                        stream=None) -> None:
+    """Append n_toks[b] new tokens to each sequence at from_toks[b]: keys with
+    the position rotation, values as they are, into the pool; queries rotated
+    into q_out.  k, v: CUDA [L][n][kv_heads][D], q: [L][n][q_heads][D], the
+    sequences' tokens one after the other; each head's row and a token's heads
+    contiguous, tokens and layers at any stride (slices of one projection's
+    output).  cos_sin: CUDA float32 [positions][rotary_dim], cosines then
+    sines (None: no rotation).  first_pos: positions of the first new tokens
+    (default: from_toks)."""
+    code, dtype = _dtype_code(k, "k"), pool.k[0].dtype
+    f, n = _host_i32(from_toks), _host_i32(n_toks)
+    if f.ndim != 1 or f.shape != n.shape:
+        raise ValueError("from_toks and n_toks must hold one number per sequence")
+    total, heads = int(n.sum(dtype=np.int64)), pool.num_kv_heads
+    rows = [(k, heads, "k"), (v, heads, "v")]
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out come together")
+    if q is not None:
+        rows.append((q, q.shape[2] if q.dim() == 4 else 0, "q"))
+        if q_out.shape != q.shape or q_out.dtype != dtype or not q_out.is_cuda or not q_out.is_contiguous():
+            raise ValueError("q_out must be a contiguous CUDA tensor of q's shape and type")
+    for t, h, name in rows:
+        if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != (pool.num_layers, total, h, pool.head_dim):
+            raise ValueError(f"{name} must be a CUDA [layers][tokens][heads][head_dim] tensor of the pool's type")
+        if total and (t.stride(3) != 1 or (h > 1 and t.stride(2) != pool.head_dim)):
+            raise ValueError(f"the heads of a token of {name} must be contiguous")
+    _device_tables(tables, f.size)
+    if cos_sin is not None and (cos_sin.dtype != torch.float32 or not cos_sin.is_cuda or not cos_sin.is_contiguous()
+                                or cos_sin.dim() != 2):
+        raise ValueError("cos_sin must be a contiguous CUDA float32 [positions][rotary_dim] tensor")
+    p = None
+    if first_pos is not None:
+        p = _host_i32(first_pos)
+        if p.shape != f.shape:
+            raise ValueError("first_pos must hold one position per sequence")
+    d = _AppendDesc(code, f.size, q.shape[2] if q is not None else 0, tables.shape[1],
+                    q.data_ptr() if q is not None else None, k.data_ptr(), v.data_ptr(),
+                    q_out.data_ptr() if q is not None else None,
+                    *_row_strides(q), *_row_strides(k), *_row_strides(v), tables.data_ptr(), f.ctypes.data, n.ctypes.data,
+                    p.ctypes.data if p is not None else None, cos_sin.data_ptr() if cos_sin is not None else None,
+                    cos_sin.shape[0] if cos_sin is not None else 0, cos_sin.shape[1] if cos_sin is not None else 0,
+                    1 if interleaved else 0)
+    _check(_lib.llmig_append_rotary(pool.handle, ctypes.byref(d), _stream(stream)), "llmig_append_rotary")
+    _used_on(stream, q, k, v, q_out, tables, cos_sin)
+
+
+def llmig_key_bounds(pool: Pool, bounds: Pool, tables: torch.Tensor, from_toks, ctx_lens, stream=None) -> None:
+    """Bring the keys' bounds up to date after tokens [from_toks[b],
+    ctx_lens[b]) of each sequence were written.  bounds: a pool of block_size
+    1 with the cache's layers, blocks, heads, head_dim and type, whose K
+    tensors take the least and V tensors the largest key of each block."""
+    code = _dtype_code(pool.k[0], "the pool")
+    if bounds.k[0].dtype != pool.k[0].dtype:
+        raise ValueError("bounds must be of the pool's type")
+    f, c = _host_i32(from_toks), _host_i32(ctx_lens)
+    if f.ndim != 1 or f.shape != c.shape:
+        raise ValueError("from_toks and ctx_lens must hold one number per sequence")
+    _device_tables(tables, f.size)
+    _check(_lib.llmig_key_bounds(pool.handle, bounds.handle, code, f.size, tables.data_ptr(), tables.shape[1],
+                                 f.ctypes.data, c.ctypes.data, _stream(stream)), "llmig_key_bounds")
+    _used_on(stream, tables)
+
+
+def select_workspace_bytes(bounds: Pool, block_size: int, ctx_lens) -> int:
+    c = _host_i32(ctx_lens)
+    n = ctypes.c_int64(0)
+    _check(_lib.llmig_select_blocks_workspace(bounds.handle, int(block_size), c.ctypes.data, c.size, ctypes.byref(n)),
+           "llmig_select_blocks_workspace")
+    return n.value
+
+
+def llmig_select_blocks(bounds: Pool, block_size: int, q: torch.Tensor, tables: torch.Tensor, ctx_lens,
+                        keep_first: int, keep_last: int, workspace: torch.Tensor, blocks: torch.Tensor,
+                        stream=None) -> None:
+    """Choose blocks for each (layer, sequence, KV head) by what their bounds
+    allow a score to reach.  q: CUDA [L][B][Hq][D]; blocks: CUDA int32
+    [L][B][kv_heads][count], ascending block numbers, then -1."""
+    code = _dtype_code(q, "q")
+    if not q.is_cuda or not q.is_contiguous() or q.dim() != 4 or q.shape[0] != bounds.num_layers or \
+            q.shape[3] != bounds.head_dim or q.dtype != bounds.k[0].dtype:
+        raise ValueError("q must be a contiguous CUDA [layers][batch][q_heads][head_dim] tensor of the bounds' type")
+    c = _host_i32(ctx_lens)
+    if c.size != q.shape[1]:
+        raise ValueError("ctx_lens must hold one length per sequence of q")
+    _device_tables(tables, c.size)
+    if blocks.dtype != torch.int32 or not blocks.is_cuda or not blocks.is_contiguous() or blocks.dim() != 4 or \
+            tuple(blocks.shape[:3]) != (bounds.num_layers, c.size, bounds.num_kv_heads):
+        raise ValueError("blocks must be a contiguous CUDA int32 [layers][batch][kv_heads][count] tensor")
+    nbytes = _workspace(workspace)
+    _check(_lib.llmig_select_blocks(bounds.handle, code, int(block_size), q.data_ptr(), c.size, q.shape[2],
+                                    tables.data_ptr(), tables.shape[1], c.ctypes.data, int(keep_first),
+                                    int(keep_last), blocks.shape[3], workspace.data_ptr(), nbytes, blocks.data_ptr(),
+                                    _stream(stream)), "llmig_select_blocks")
+    _used_on(stream, q, tables, workspace, blocks)
+
+
+def decode_blocks_workspace_bytes(pool: Pool, ctx_lens, q_heads: int, count: int) -> int:
+    c = _host_i32(ctx_lens)
+    n = ctypes.c_int64(0)
+    _check(_lib.llmig_decode_attention_blocks_workspace(pool.handle, c.ctypes.data, c.size, int(q_heads), int(count),
+                                                        ctypes.byref(n)), "llmig_decode_attention_blocks_workspace")
+    return n.value
+
+
+def llmig_decode_attention_blocks(pool: Pool, q: torch.Tensor, tables: torch.Tensor, ctx_lens, blocks: torch.Tensor,
+                                  scale: float, workspace: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    """llmig_decode_attention of each (layer, sequence, KV head) over the
+    blocks that blocks (CUDA int32 [L][B][kv_heads][count]) lists for it."""
+    c = _attention_args(pool, q, tables, ctx_lens, out)
+    nbytes = _workspace(workspace)
+    if blocks.dtype != torch.int32 or not blocks.is_cuda or not blocks.is_contiguous() or blocks.dim() != 4 or \
+            tuple(blocks.shape[:3]) != (pool.num_layers, q.shape[1], pool.num_kv_heads):
+        raise ValueError("blocks must be a contiguous CUDA int32 [layers][batch][kv_heads][count] tensor")
+    _check(_lib.llmig_decode_attention_blocks(pool.handle, 1 if q.dtype == torch.bfloat16 else 0, q.data_ptr(),
+                                              q.shape[1], q.shape[2], tables.data_ptr(), tables.shape[1],
+                                              c.ctypes.data, blocks.data_ptr(), blocks.shape[3], float(scale),
+                                              workspace.data_ptr(), nbytes, out.data_ptr(), _stream(stream)),
+           "llmig_decode_attention_blocks")
+    _used_on(stream, q, tables, blocks, workspace, out)
+
+
+def decode_prefix_workspace_bytes(pool: Pool, ctx_lens, q_heads: int, prefix_blocks: int) -> int:
+    c = _host_i32(ctx_lens)
+    n = ctypes.c_int64(0)
+    _check(_lib.llmig_decode_attention_prefix_workspace(pool.handle, c.ctypes.data, c.size, int(q_heads),
+                                                        int(prefix_blocks), ctypes.byref(n)),
+           "llmig_decode_attention_prefix_workspace")
+    return n.value
+
+
+def llmig_decode_attention_prefix(pool: Pool, q: torch.Tensor, tables: torch.Tensor, ctx_lens, prefix_blocks: int,
+                                  scale: float, workspace: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    """llmig_decode_attention of a batch whose table rows begin with the same
+    prefix_blocks blocks: those are read once for all sequences."""
+    c = _attention_args(pool, q, tables, ctx_lens, out)
+    nbytes = _workspace(workspace)
+    _check(_lib.llmig_decode_attention_prefix(pool.handle, 1 if q.dtype == torch.bfloat16 else 0, q.data_ptr(),
+                                              q.shape[1], q.shape[2], tables.data_ptr(), tables.shape[1],
+                                              c.ctypes.data, int(prefix_blocks), float(scale), workspace.data_ptr(),
+                                              nbytes, out.data_ptr(), _stream(stream)), "llmig_decode_attention_prefix")
+    _used_on(stream, q, tables, workspace, out)

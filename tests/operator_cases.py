@@ -1,0 +1,112 @@
+"""Plain references in 64 bits, and error bounds, for the operators of a decode
+step over long contexts.  Everything is computed on the CPU from the 16-bit
+inputs as they are.
+
+Bound of an attention output (the reasoning is that of tests/attn_cases.py),
+for a row of n tokens, u = 2^-24 and lambda = 8:
+
+    tol = A (eps_p + lambda u (2 sqrt(depth) + 4 (sqrt(D) + 2) S + 2)) + lambda sqrt(n) u_lo / W + u
+
+A the softmax-weighted mean of |v|, eps_p = 2^-16 (bf16) or 2^-22 (fp16) the
+weights' error as a 16-bit high and a 16-bit low part, depth = 64 + ceil(n / 16)
+at least the longest chain of fp32 additions (a matrix product adds 32 terms, a
+wavefront takes at most every 16-token group, then wavefronts and partitions
+join, fewer than 32 of them), S a bound on |score| (here |k| is not bounded by
+1, so it is the largest sum_d |q_d k_d|, scaled), u_lo = 2^-25 for fp16 (the
+low part's absolute rounding; 0 for bf16), W the weights' sum relative to the
+largest."""
+from __future__ import annotations
+
+import math
+
+import torch
+
+LAMBDA, U32 = 8.0, 2.0 ** -24
+TYPES = {"fp16": torch.float16, "bf16": torch.bfloat16}
+EPS_P = {"fp16": 2.0 ** -22, "bf16": 2.0 ** -16}
+HALF_STEP = {"fp16": 2.0 ** -11, "bf16": 2.0 ** -8}     # of one rounding to the type, relative
+
+
+def rows_of(tables, b, tokens, bs):
+    """(block, slot) of the listed tokens of sequence b."""
+    t = torch.as_tensor(tokens, dtype=torch.long)
+    return tables[b].long()[t // bs], t % bs
+
+
+def attention(k, v, q, scale, dtype):
+    """One row: k, v [n][D], q [G][D] (any type): (out [G][D], tol [G][D])."""
+    G, D = q.shape
+    n = k.shape[0]
+    if n == 0:
+        return torch.zeros(G, D, dtype=torch.float64), torch.zeros(G, D, dtype=torch.float64)
+    k, v, q = k.double(), v.double(), q.double()
+    s = (q @ k.t()) * scale
+    out = torch.zeros(G, D, dtype=torch.float64)
+    tol = torch.full((G, D), U32, dtype=torch.float64)
+    for g in range(G):
+        if bool(torch.isnan(s[g]).any()) or bool((s[g] == math.inf).any()) or not bool(torch.isfinite(s[g]).any()):
+            tol[g] = 0.0            # zeros, exactly
+            continue
+        live = s[g] > -math.inf
+        w = torch.exp(s[g][live] - s[g].max())
+        W = w.sum()
+        out[g] = (w @ v[live]) / W
+        A = (w @ v[live].abs()) / W
+        S = abs(scale) * float((q[g].abs() * k[live].abs()).sum(1).max())
+        rel = EPS_P[dtype] + LAMBDA * U32 * (2 * math.sqrt(64 + -(-n // 16)) + 4 * (math.sqrt(D) + 2) * S + 2)
+        lo = LAMBDA * math.sqrt(n) * U32 / 2 / float(W) * float(v[live].abs().max()) if dtype == "fp16" else 0.0
+        tol[g] = A * rel + lo + U32
+    return out, tol
+
+
+def decode(kv, q, tables, scale, dtype, tokens_of):
+    """kv [2][L][blocks][bs][H][D], q [L][B][Hq][D] on the CPU; tokens_of(l, b, g)
+    lists the tokens a row attends to."""
+    L, B, HQ, D = q.shape
+    bs, H = kv.shape[3], kv.shape[4]
+    G = HQ // H
+    out, tol = torch.zeros(q.shape, dtype=torch.float64), torch.zeros(q.shape, dtype=torch.float64)
+    for l in range(L):
+        for b in range(B):
+            for g in range(H):
+                blk, slot = rows_of(tables, b, tokens_of(l, b, g), bs)
+                at = slice(g * G, (g + 1) * G)
+                out[l, b, at], tol[l, b, at] = attention(kv[0, l, blk, slot, g], kv[1, l, blk, slot, g], q[l, b, at],
+                                                         scale, dtype)
+    return out, tol
+
+
+def rotate(x, cos, sin, interleaved):
+    """x [..., D] float64, cos and sin [..., h]."""
+    h = cos.shape[-1]
+    y = x.clone()
+    a, b = (slice(0, 2 * h, 2), slice(1, 2 * h, 2)) if interleaved else (slice(0, h), slice(h, 2 * h))
+    y[..., a] = x[..., a] * cos - x[..., b] * sin
+    y[..., b] = x[..., b] * cos + x[..., a] * sin
+    return y
+
+
+def select(lo, hi, q, n, keep_first, keep_last, count):
+    """lo, hi [n][H][D], q [Hq][D]: lists [H][count]."""
+    H = lo.shape[1]
+    G = q.shape[0] // H
+    out = torch.full((H, count), -1, dtype=torch.int32)
+    for g in range(H):
+        x = q[g * G:(g + 1) * G].double()
+        score = (x.clamp(min=0).sum(0) * hi[:, g].double() + x.clamp(max=0).sum(0) * lo[:, g].double()).sum(-1)
+        score = [math.inf if math.isnan(s) else s for s in score.tolist()]
+        must = [j for j in range(n) if j < keep_first or j >= n - keep_last]
+        rest = sorted((j for j in range(n) if j not in set(must)), key=lambda j: (-score[j], j))
+        chosen = sorted((must + rest)[:min(count, n)])
+        out[g, :len(chosen)] = torch.tensor(chosen, dtype=torch.int32)
+    return out
+
+
+def worst(got, want, tol):
+    """Largest |got - want| / tol; infinite where one is not finite, or an
+    exact value is missed."""
+    got = got.double().cpu()
+    err = (got - want).abs()
+    ratio = torch.where(tol > 0, err / tol.clamp(min=1e-300), torch.where(err > 0, math.inf, 0.0))
+    ratio = torch.where(torch.isfinite(got), ratio, torch.tensor(math.inf, dtype=torch.float64))
+    return float(ratio.max()) if ratio.numel() else 0.0
