@@ -82,18 +82,24 @@ struct SelectArgs {
     const uint64_t *tab;         // the bounds' table: least (K) then largest (V) bases
     const uint8_t *q;            // [L][B][Hq][D]
     const int32_t *tables;
-    uint64_t *keys;              // [L][sum of n_s][H]: the scores, as words of the same order
+    uint64_t *keys;              // the scores, as words of the same order: [L][sequence][H][its blocks]
     int32_t *out;                // [L][B][H][count]
     uint32_t num_layers, num_blocks, batch, q_heads, kv_heads, table_stride;
     uint32_t keep_first, keep_last, count;
     uint32_t blocks;             // sum of the sequences' blocks
     uint32_t first_item;         // this launch's first item
+    uint32_t per_row;            // score_blocks: blocks that a row of lanes takes, one after the other
     uint32_t parts;              // score_blocks: workgroups of the longest sequence, one layer and slice
     uint32_t slices;             // score_blocks: 256-lane slices of a row of bounds
     uint32_t block_end[kAppendMaxBatch];  // blocks of the first s + 1 sequences
 };
 
-constexpr uint32_t kScoreBlocks = 32;     // blocks that a row of lanes of score_blocks takes one after the other
+// Where the keys of (layer, sequence, KV head) start; `first` blocks of other
+// sequences come before the sequence's n.
+__device__ __forceinline__ uint64_t key_row(const SelectArgs &a, uint32_t layer, uint32_t first, uint32_t n, uint32_t g)
+{
+    return (static_cast<uint64_t>(layer) * a.blocks + first) * a.kv_heads + static_cast<uint64_t>(g) * n;
+}
 
 // A score as a word: unsigned order is the scores' order, NaN is the highest
 // (a block whose bounds say nothing is not left out), and -0 equals 0.
@@ -107,7 +113,11 @@ __device__ __forceinline__ uint64_t score_key(double x)
 }
 
 // A lane takes 8 dims of one KV head, its sums P and N in registers, over the
-// blocks of its part; the D / 8 lanes of a head add up.
+// consecutive blocks of its row of lanes, kScoreAhead blocks' bounds in flight;
+// the D / 8 lanes of a head add up, and each keeps the score of one block in
+// D / 8, so that scores leave as whole lines.
+constexpr uint32_t kScoreAhead = 4;
+
 template <int BF16, int D>
 __global__ void __launch_bounds__(kThreads) score_blocks(const SelectArgs a)
 {
@@ -124,11 +134,10 @@ __global__ void __launch_bounds__(kThreads) score_blocks(const SelectArgs a)
     const uint32_t rows = row < kThreads ? kThreads / row : 1u;    // rows of lanes in the workgroup
     const uint32_t r = row < kThreads ? threadIdx.x / row : 0u;
     const uint32_t chunk = row < kThreads ? threadIdx.x % row : slice * kThreads + threadIdx.x;
-    const uint32_t j0 = part * rows * kScoreBlocks;
-    if (n <= a.count || j0 >= n)       // every block of a short sequence is listed
+    if (n <= a.count || part * rows * a.per_row >= n)      // every block of a short sequence is listed
         return;
     const bool in = r < rows && chunk < row;
-    const uint32_t head = in ? chunk / C : 0u, c = in ? chunk % C : 0u;
+    const uint32_t head = in ? chunk / C : 0u, c = threadIdx.x % C;
     const uint32_t G = a.q_heads / a.kv_heads;
     double p[8], m[8];
 #pragma unroll
@@ -145,35 +154,114 @@ __global__ void __launch_bounds__(kThreads) score_blocks(const SelectArgs a)
     }
     const uint8_t *lo = reinterpret_cast<const uint8_t *>(table_entry(a.tab, layer));
     const uint8_t *hi = reinterpret_cast<const uint8_t *>(table_entry(a.tab, a.num_layers + layer));
-    for (uint32_t k = 0; k < kScoreBlocks; ++k) {
-        const uint32_t j = j0 + k * rows + r;
-        if (j0 + k * rows >= n)
-            break;
-        const bool here = in && j < n;
-        double sum = 0.0;
-        if (here) {
-            const uint32_t id = min(table_id(a.tables, s, a.table_stride, j), a.num_blocks - 1u);
-            const uint64_t at = (static_cast<uint64_t>(id) * row + chunk) * 16u;
-            float x[8], y[8];
-            unpack8<BF16>(load16(hi + at), x);
-            unpack8<BF16>(load16(lo + at), y);
+    const uint32_t j0 = (part * rows + (in ? r : 0u)) * a.per_row;
+    uint64_t *out = a.keys + key_row(a, layer, first, n, head);
+    uint64_t kept = 0;
+    for (uint32_t k0 = 0; k0 < a.per_row; k0 += kScoreAhead) {
+        u32x4 x[kScoreAhead], y[kScoreAhead];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                sum += p[e] * static_cast<double>(x[e]) + m[e] * static_cast<double>(y[e]);
+        for (uint32_t u = 0; u < kScoreAhead; ++u) {
+            const uint32_t j = min(j0 + k0 + u, n - 1u);
+            const uint32_t id = min(table_id(a.tables, s, a.table_stride, j), a.num_blocks - 1u);
+            const uint64_t at = (static_cast<uint64_t>(id) * row + (in ? chunk : 0u)) * 16u;
+            x[u] = load16(hi + at);
+            y[u] = load16(lo + at);
         }
 #pragma unroll
-        for (uint32_t d = 1; d < C; d *= 2)
-            sum += __shfl_xor(sum, d);
-        if (here && c == 0)
-            a.keys[(static_cast<uint64_t>(layer) * a.blocks + first + j) * a.kv_heads + head] = score_key(sum);
+        for (uint32_t u = 0; u < kScoreAhead; ++u) {
+            float up[8], low[8];
+            unpack8<BF16>(x[u], up);
+            unpack8<BF16>(y[u], low);
+            double sum = 0.0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                sum += p[e] * static_cast<double>(up[e]) + m[e] * static_cast<double>(low[e]);
+#pragma unroll
+            for (uint32_t d = 1; d < C; d *= 2)
+                sum += __shfl_xor(sum, d);
+            if (c == (k0 + u) % C)
+                kept = score_key(sum);
+        }
+        const uint32_t done = k0 + kScoreAhead;             // per_row is a multiple of C, or less than C
+        if (done % C == 0 || done >= a.per_row) {
+            const uint32_t j = j0 + (done - 1u) / C * C + c;
+            if (in && j < j0 + min(done, a.per_row) && j < n)
+                out[j] = kept;
+        }
     }
+}
+
+// Blocks of a row of lanes, for `work` rows of lanes times blocks in all:
+// enough workgroups to fill the chip before a row of lanes takes more than it
+// can have in flight.
+inline uint32_t score_blocks_per_row(uint64_t work)
+{
+    return work >= 16 * 2048 ? 16 : work >= 8 * 1024 ? 8 : 4;
+}
+
+// The parallel part of a pass of the search below: of the counts of 256 bins,
+// which one holds the need-th key from the top, and how many of it are needed.
+// Needs kThreads threads at least; the first 256 hold a bin each.
+__device__ __forceinline__ void find_bin(uint32_t *bins, uint32_t *wave_sum, uint32_t *found, uint32_t need)
+{
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    uint32_t mine = 0, sum = 0;
+    if (threadIdx.x < 256) {
+        mine = sum = bins[255u - threadIdx.x];       // from the top
+#pragma unroll
+        for (uint32_t d = 1; d < 64; d *= 2) {
+            const uint32_t v = __shfl_up(sum, d);
+            sum += lane >= d ? v : 0u;
+        }
+        if (lane == 63)
+            wave_sum[wave] = sum;
+    }
+    __syncthreads();
+    if (threadIdx.x < 256) {
+        for (uint32_t x = 0; x < wave; ++x)
+            sum += wave_sum[x];
+        if (sum >= need && sum - mine < need) {
+            found[0] = 255u - threadIdx.x;
+            found[1] = need - (sum - mine);          // needed of the bin
+            found[2] = mine;                         // keys in it
+        }
+        bins[255u - threadIdx.x] = 0;
+    }
+    __syncthreads();
+}
+
+// Makes x[0 .. N) the sums of what comes before each entry.
+template <uint32_t N>
+__device__ __forceinline__ void exclusive_sums(uint32_t *x)
+{
+    if (threadIdx.x < 64) {
+        uint32_t before = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < N; k += 64) {
+            const uint32_t at = k + threadIdx.x, v = at < N ? x[at] : 0u;
+            uint32_t sum = v;
+#pragma unroll
+            for (uint32_t d = 1; d < 64; d *= 2) {
+                const uint32_t y = __shfl_up(sum, d);
+                sum += threadIdx.x >= d ? y : 0u;
+            }
+            if (at < N)
+                x[at] = before + sum - v;
+            before += __shfl(sum, 63);
+        }
+    }
+    __syncthreads();
 }
 
 // Lists the `count` highest keys of a row (layer, sequence, KV head), one
 // workgroup a row: a radix search for the key of the last one listed, a byte a
-// pass, then one walk through the blocks in order.
-__global__ void __launch_bounds__(kThreads) list_blocks(const SelectArgs a)
+// pass, which ends as soon as all keys that begin alike are listed; then the
+// listed ones leave in order.  KPT: a thread holds that many keys, which are
+// read once; 0: rows too long for that read them from memory in each pass.
+template <int T, int KPT>
+__global__ void __launch_bounds__(T) list_blocks(const SelectArgs a)
 {
+    constexpr uint32_t kWaves = T / 64, kHeld = KPT ? KPT : 1;
     uint32_t w = a.first_item + blockIdx.x;
     const uint32_t g = w % a.kv_heads;
     w /= a.kv_heads;
@@ -182,75 +270,135 @@ __global__ void __launch_bounds__(kThreads) list_blocks(const SelectArgs a)
     const uint32_t n = a.block_end[s] - first;
     int32_t *out = a.out + ((static_cast<uint64_t>(layer) * a.batch + s) * a.kv_heads + g) * a.count;
     if (n <= a.count) {
-        for (uint32_t k = threadIdx.x; k < a.count; k += kThreads)
+        for (uint32_t k = threadIdx.x; k < a.count; k += T)
             out[k] = k < n ? static_cast<int32_t>(k) : -1;
         return;
     }
-    const uint64_t *keys = a.keys + (static_cast<uint64_t>(layer) * a.blocks + first) * a.kv_heads + g;
+    const uint64_t *keys = a.keys + key_row(a, layer, first, n, g);
     // blocks that are always listed stand above every score (count holds them)
-    auto key = [&](uint32_t j) {
-        return j < a.keep_first || j >= n - a.keep_last ? ~0ull : keys[static_cast<uint64_t>(j) * a.kv_heads];
+    auto key_of = [&](uint32_t j) {
+        return j < a.keep_first || j >= n - a.keep_last ? ~0ull : keys[j];
     };
-    __shared__ uint32_t bins[256];
-    __shared__ uint32_t sh_bin, sh_need;
-    __shared__ uint32_t wave_sum[2][kThreads / 64];
+    __shared__ uint32_t bins[256], wave_sum[kWaves], found[3];
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    uint64_t held[kHeld];
+    if constexpr (KPT > 0)
+#pragma unroll
+        for (uint32_t i = 0; i < KPT; ++i) {
+            const uint32_t j = i * T + threadIdx.x;
+            held[i] = j < n ? key_of(j) : 0ull;      // (no score's key: those of -inf are above it)
+        }
+    auto each = [&](auto &&f) {
+        if constexpr (KPT > 0) {
+#pragma unroll
+            for (uint32_t i = 0; i < KPT; ++i)
+                f(i * T + threadIdx.x, held[i]);
+        } else {
+            for (uint32_t j = threadIdx.x; j < n; j += T)
+                f(j, key_of(j));
+        }
+    };
+    if (threadIdx.x < 256)
+        bins[threadIdx.x] = 0;
+    __syncthreads();
     uint64_t prefix = 0;
     uint32_t need = a.count;           // of the keys that begin with prefix, these many are listed
-    for (int shift = 56; shift >= 0; shift -= 8) {
-        bins[threadIdx.x] = 0;
-        __syncthreads();
-        for (uint32_t j = threadIdx.x; j < n; j += kThreads) {
-            const uint64_t k = key(j);
-            if (shift == 56 || k >> (shift + 8) == prefix)
+    int shift = 56;
+    bool ties = true;                  // whether not all of them are
+    for (; shift >= 0 && ties; shift -= 8) {
+        each([&](uint32_t j, uint64_t k) {
+            if (j < n && (shift == 56 || k >> (shift + 8) == prefix))
                 atomicAdd(&bins[static_cast<uint32_t>(k >> shift) & 255u], 1u);
-        }
+        });
         __syncthreads();
-        if (threadIdx.x == 0) {
-            uint32_t b = 255, left = need;
-            while (b > 0 && bins[b] < left) {
-                left -= bins[b];
-                --b;
-            }
-            sh_bin = b;
-            sh_need = left;
-        }
-        __syncthreads();
-        prefix = prefix << 8 | sh_bin;
-        need = sh_need;
-        __syncthreads();
+        find_bin(bins, wave_sum, found, need);
+        prefix = prefix << 8 | found[0];
+        need = found[1];
+        ties = found[1] != found[2];
     }
-    // in order: every key above the last one listed, and the first `need` equal to it
-    uint32_t listed = 0, equal = 0;
-    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-    for (uint32_t j0 = 0; j0 < n; j0 += kThreads) {
-        const uint32_t j = j0 + threadIdx.x;
-        const uint64_t k = j < n ? key(j) : 0ull;
-        const bool above = j < n && k > prefix, same = j < n && k == prefix;
-        const uint64_t below = (1ull << lane) - 1ull;
-        const uint64_t same_mask = __ballot(same);
-        if (lane == 0)
-            wave_sum[0][wave] = __popcll(same_mask);
-        __syncthreads();
-        uint32_t rank = equal + __popcll(same_mask & below), all_same = 0;
-        for (uint32_t x = 0; x < kThreads / 64; ++x) {
-            rank += x < wave ? wave_sum[0][x] : 0u;
-            all_same += wave_sum[0][x];
+    shift += 8;
+    // every key that begins above prefix, and the first `need` that begin with it
+    const uint64_t below = (1ull << lane) - 1ull;
+    if constexpr (KPT > 0) {
+        __shared__ uint32_t chunk[KPT * kWaves];     // of 64 blocks each, in order
+        uint32_t take = 0, same = 0;                 // a bit per key held
+#pragma unroll
+        for (uint32_t i = 0; i < KPT; ++i) {
+            const uint64_t top = held[i] >> shift;
+            if (i * T + threadIdx.x < n && top >= prefix) {
+                take |= 1u << i;
+                same |= top == prefix ? 1u << i : 0u;
+            }
         }
-        const bool take = above || (same && rank < need);
+        auto rank = [&](uint32_t flags, auto &&f) {
+#pragma unroll
+            for (uint32_t i = 0; i < KPT; ++i) {
+                const uint64_t mask = __ballot(flags >> i & 1u);
+                if (lane == 0)
+                    chunk[i * kWaves + wave] = __popcll(mask);
+            }
+            __syncthreads();
+            exclusive_sums<KPT * kWaves>(chunk);
+#pragma unroll
+            for (uint32_t i = 0; i < KPT; ++i) {
+                const uint64_t mask = __ballot(flags >> i & 1u);
+                f(i, chunk[i * kWaves + wave] + static_cast<uint32_t>(__popcll(mask & below)));
+            }
+        };
+        if (ties) {
+            uint32_t kept = take & ~same;
+            rank(same, [&](uint32_t i, uint32_t at) { kept |= at < need ? same & 1u << i : 0u; });
+            take = kept;
+            __syncthreads();
+        }
+        rank(take, [&](uint32_t i, uint32_t at) {
+            if (take >> i & 1u)
+                out[at] = static_cast<int32_t>(i * T + threadIdx.x);
+        });
+        return;
+    }
+    __shared__ uint32_t sums[2][kWaves];
+    uint32_t listed = 0, equal = 0;
+    for (uint32_t i = 0; i * T < n; ++i) {
+        const uint32_t j = i * T + threadIdx.x;
+        const uint64_t top = (j < n ? key_of(j) : 0ull) >> shift;
+        const bool same = j < n && top == prefix;
+        bool take = j < n && top >= prefix;
+        if (ties) {
+            const uint64_t same_mask = __ballot(same);
+            if (lane == 0)
+                sums[0][wave] = __popcll(same_mask);
+            __syncthreads();
+            uint32_t rank = equal + __popcll(same_mask & below);
+            for (uint32_t x = 0; x < kWaves; ++x) {
+                rank += x < wave ? sums[0][x] : 0u;
+                equal += sums[0][x];
+            }
+            take = take && (!same || rank < need);
+        }
         const uint64_t take_mask = __ballot(take);
         if (lane == 0)
-            wave_sum[1][wave] = __popcll(take_mask);
+            sums[1][wave] = __popcll(take_mask);
         __syncthreads();
-        uint32_t at = listed + __popcll(take_mask & below), all_take = 0;
-        for (uint32_t x = 0; x < kThreads / 64; ++x) {
-            at += x < wave ? wave_sum[1][x] : 0u;
-            all_take += wave_sum[1][x];
+        uint32_t at = listed + __popcll(take_mask & below);
+        for (uint32_t x = 0; x < kWaves; ++x) {
+            at += x < wave ? sums[1][x] : 0u;
+            listed += sums[1][x];
         }
         if (take)
             out[at] = static_cast<int32_t>(j);
-        listed += all_take;
-        equal += all_same;
+        __syncthreads();
     }
+}
+
+// The kernel for rows of at most `longest` blocks, and its threads.
+inline const void *list_kernel(uint32_t longest, uint32_t *threads)
+{
+    *threads = longest <= 4096 ? 256 : 1024;
+    return longest <= 1024    ? reinterpret_cast<const void *>(&list_blocks<256, 4>)
+           : longest <= 4096  ? reinterpret_cast<const void *>(&list_blocks<256, 16>)
+           : longest <= 16384 ? reinterpret_cast<const void *>(&list_blocks<1024, 16>)
+                              : reinterpret_cast<const void *>(&list_blocks<1024, 0>);
 }
 
 } // namespace

@@ -1412,13 +1412,14 @@ int llmig_decode_attention_noalloc(const llmig_pool *pool, int32_t dtype, const 
 // Launches `fn` on items 0 .. items - 1 of a call, one workgroup an item, in
 // launches that the grid can hold; `first` is set to a launch's first item, in
 // units of `per` items.
-static int launch_items(const void *fn, void *args, uint64_t items, uint32_t per, uint32_t *first, hipStream_t st)
+static int launch_items(const void *fn, void *args, uint64_t items, uint32_t per, uint32_t *first, hipStream_t st,
+                        uint32_t threads = kThreads)
 {
     const uint64_t step = std::max<uint64_t>(kMaxGridWorkgroups / per, 1) * per;
     for (uint64_t at = 0; at < items; at += step) {
         *first = static_cast<uint32_t>(at / per);
         void *list[] = {args};
-        const hipError_t e = hipLaunchKernel(fn, dim3(static_cast<uint32_t>(std::min(step, items - at))), dim3(kThreads),
+        const hipError_t e = hipLaunchKernel(fn, dim3(static_cast<uint32_t>(std::min(step, items - at))), dim3(threads),
                                              list, 0, st);
         if (e != hipSuccess)
             return hip_error(e);
@@ -1704,8 +1705,9 @@ int llmig_select_blocks(const llmig_pool *bounds, int32_t dtype, int32_t block_s
     a.keep_last = static_cast<uint32_t>(keep_last);
     a.count = static_cast<uint32_t>(count);
     a.blocks = static_cast<uint32_t>(n);
-    a.parts = std::max(1u, (longest + rows * kScoreBlocks - 1) / (rows * kScoreBlocks));
     a.slices = (row + kThreads - 1) / kThreads;
+    a.per_row = score_blocks_per_row(a.num_layers * static_cast<uint64_t>(n) * a.slices / rows);
+    a.parts = std::max(1u, (longest + rows * a.per_row - 1) / (rows * a.per_row));
     const uint64_t lists = static_cast<uint64_t>(a.num_layers) * a.batch * a.kv_heads;
     const uint64_t items = static_cast<uint64_t>(a.num_layers) * a.batch * a.slices * a.parts;
     if (n > 0x7fffffffLL || items > 0x7fffffffull || lists > 0x7fffffffull)
@@ -1721,7 +1723,9 @@ int llmig_select_blocks(const llmig_pool *bounds, int32_t dtype, int32_t block_s
         if (rc != LLMIG_OK)
             return rc;
     }
-    return launch_items(reinterpret_cast<const void *>(&list_blocks), &a, lists, 1, &a.first_item, st);
+    uint32_t threads = 0;
+    const void *list = list_kernel(longest, &threads);
+    return launch_items(list, &a, lists, 1, &a.first_item, st, threads);
 }
 
 int llmig_decode_attention_blocks_workspace(const llmig_pool *pool, const int32_t *ctx_lens, int32_t batch,

@@ -61,6 +61,27 @@ __device__ __forceinline__ float sum_of_rows(float x)
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// Two weights as their 16-bit roundings and the 16-bit roundings of what these
+// leave, the first weight in the low halves.
+template <int BF16>
+__device__ __forceinline__ void split_weights(float p0, float p1, uint32_t *hi, uint32_t *lo)
+{
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    if constexpr (BF16) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
+        *hi = h;
+        *lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - __uint_as_float(h << 16),
+                                                                          p1 - __uint_as_float(h & 0xffff0000u)}), bf16x2));
+    } else {
+        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+        const f16x2 h = __builtin_convertvector((f32x2{p0, p1}), f16x2);
+        *hi = __builtin_bit_cast(uint32_t, h);
+        *lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - static_cast<float>(h.x),
+                                                                          p1 - static_cast<float>(h.y)}), f16x2));
+    }
+}
+
 // One workgroup: a partition of one (layer, KV head) against 32 * WM query
 // rows.  Of its four wavefronts WM split the rows, 32 each (two MFMA columns
 // of 16), and 4 / WM the tokens of each tile.
@@ -113,23 +134,32 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
         const uint32_t r = min(row0 + 16u * rt + r16, M - 1u);
         const uint64_t q_row = (static_cast<uint64_t>(layer) * a.batch + a.member[r / G]) * a.q_heads + g * G + r % G;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-            qf[rt][ks] = load16(a.q + (q_row * D + 32 * ks + 8 * g4) * 2);
+        for (int ks = 0; ks < KS; ++ks) {
+            // a negative scale: the queries' signs turn, so that scores rise
+            // with their products
+            qf[rt][ks] = load16(a.q + (q_row * D + 32 * ks + 8 * g4) * 2) ^ (a.scale < 0.f ? 0x80008000u : 0u);
+        }
     }
 
     // A tile's rows: thread's chunk of token th + i * (kThreads / LPR), brought
-    // into registers while the tile before it is worked on.  Tokens past the
-    // partition's end repeat its last one; their scores are masked.
+    // into registers while the tile before it is worked on, and their blocks'
+    // ids one tile ahead of them.  Tokens past the partition's end repeat its
+    // last one; they weigh 0.
     const uint32_t th = threadIdx.x / LPR, tc = threadIdx.x % LPR;
     u32x4 kr[CPT], vr[CPT];
+    uint32_t ids[CPT];
+    auto token_of = [&](uint32_t t0, int i) { return min(t0 + th + i * (kThreads / LPR), t_end - 1u); };
+    auto look_up = [&](uint32_t t0) {
+#pragma unroll
+        for (int i = 0; i < CPT; ++i)
+            ids[i] = static_cast<uint32_t>(a.table[divide(token_of(t0, i), a.by_block)]);
+    };
     auto fetch = [&](uint32_t t0) {
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
-            const uint32_t t = min(t0 + th + i * (kThreads / LPR), t_end - 1u);
-            const uint32_t blk = divide(t, a.by_block);
-            const uint32_t id = min(static_cast<uint32_t>(a.table[blk]), a.num_blocks - 1u);
-            const uint64_t at = ((static_cast<uint64_t>(id) * a.block_size + (t - blk * a.block_size)) * a.kv_heads + g) * RB +
-                                16u * tc;
+            const uint32_t t = token_of(t0, i), blk = divide(t, a.by_block);
+            const uint64_t slot = static_cast<uint64_t>(min(ids[i], a.num_blocks - 1u)) * a.block_size + (t - blk * a.block_size);
+            const uint64_t at = (slot * a.kv_heads + g) * RB + 16u * tc;
             kr[i] = *(const LLMIG_GLOBAL u32x4 *)(kbase + at);
             vr[i] = *(const LLMIG_GLOBAL u32x4 *)(vbase + at);
         }
@@ -146,7 +176,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
         }
     };
 
-    const float qk_scale = a.scale * kLog2e;
+    const float qk_scale = fabsf(a.scale) * kLog2e;
     float m[2] = {-INFINITY, -INFINITY}, lsum[2] = {0.f, 0.f};
     f32x4_t acc[2][MT];
 #pragma unroll
@@ -155,14 +185,19 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
         for (int mt = 0; mt < MT; ++mt)
             acc[rt][mt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
+    look_up(t_begin);
     fetch(t_begin);
+    look_up(t_begin + kPrefixTile);
     put(0);
     uint32_t buf = 0;
     for (uint32_t t0 = t_begin; t0 < t_end; t0 += kPrefixTile, buf ^= 1u) {
         __syncthreads();                      // the tile is in LDS, and the one before it is done with
         const bool more = t0 + kPrefixTile < t_end;
-        if (more)
+        if (more) {
             fetch(t0 + kPrefixTile);
+            look_up(t0 + 2 * kPrefixTile);
+        }
+        const bool tail = t0 + kPrefixTile > t_end;
         const uint8_t *kt = smem[buf][0], *vt = smem[buf][1];
 #pragma unroll
         for (int step = 0; step < TT; step += STEP) {
@@ -184,17 +219,23 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
             // tokens tb + 16 * u + 4 * g4 + i.  The maximum that weights are
             // taken against moves only when a score exceeds it by 2^8: the
             // sums have the room, and the accumulators are rescaled seldom.
-            uint64_t ph[2][STEP], pl[2][STEP];
-#pragma unroll
-            for (int rt = 0; rt < 2; ++rt) {
-                float z[STEP][4], mx = -INFINITY;
+            uint32_t ph[2][STEP][2], pl[2][STEP][2];
+            if (tail)
 #pragma unroll
                 for (int u = 0; u < STEP; ++u)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        z[u][i] = t0 + tb + 16u * u + 4u * g4 + i < t_end ? s[rt][u][i] * qk_scale : -INFINITY;
-                        mx = fmaxf(mx, z[u][i]);
-                    }
+                    for (int i = 0; i < 4; ++i)
+                        if (t0 + tb + 16u * u + 4u * g4 + i >= t_end)
+                            s[0][u][i] = s[1][u][i] = -INFINITY;
+#pragma unroll
+            for (int rt = 0; rt < 2; ++rt) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < STEP; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        mx = fmaxf(mx, s[rt][u][i]);
+                mx *= qk_scale;
                 if (__ballot(mx > m[rt] + 8.f)) {
                     const float m_new = fmaxf(m[rt], max_of_rows(mx));
                     const float c = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[rt] - m_new);
@@ -207,15 +248,17 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
                 const float m_sub = m[rt] == -INFINITY ? 0.f : m[rt];
 #pragma unroll
                 for (int u = 0; u < STEP; ++u) {
-                    ph[rt][u] = pl[rt][u] = 0;
+                    float p[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float p = __builtin_amdgcn_exp2f(z[u][i] - m_sub);
-                        lsum[rt] += p;
-                        const uint32_t hi = round16<BF16>(p);
-                        ph[rt][u] |= static_cast<uint64_t>(hi) << (16 * i);
-                        pl[rt][u] |= static_cast<uint64_t>(round16<BF16>(p - from16<BF16>(hi))) << (16 * i);
-                    }
+                    for (int i = 0; i < 4; ++i)
+                        p[i] = __builtin_amdgcn_exp2f(s[rt][u][i] * qk_scale - m_sub);
+                    if (tail)       // (a scale of 0 would make NaN of the mask's -inf)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            p[i] = t0 + tb + 16u * u + 4u * g4 + i < t_end ? p[i] : 0.f;
+                    lsum[rt] += (p[0] + p[1]) + (p[2] + p[3]);
+                    split_weights<BF16>(p[0], p[1], &ph[rt][u][0], &pl[rt][u][0]);
+                    split_weights<BF16>(p[2], p[3], &ph[rt][u][1], &pl[rt][u][1]);
                 }
             }
             // O^T += V^T . P^T, the weights as their 16-bit rounding and the
@@ -231,14 +274,15 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
                         (LLMIG_LDS i16x4_t *)(vt + t * RB + 16u * (c ^ swz(t)) + 8u * (r16 % 2u))));
                 }
                 typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+                const u32x4 v = __builtin_bit_cast(u32x4, u64x2{vf[0], vf[STEP - 1]});
 #pragma unroll
                 for (int rt = 0; rt < 2; ++rt) {
+                    const uint32_t(&h)[STEP][2] = ph[rt], (&l)[STEP][2] = pl[rt];
                     if constexpr (STEP == 2) {
-                        const u32x4 v = __builtin_bit_cast(u32x4, u64x2{vf[0], vf[1]});
-                        acc[rt][mt] = mfma_qk<BF16>(v, __builtin_bit_cast(u32x4, u64x2{ph[rt][0], ph[rt][1]}), acc[rt][mt]);
-                        acc[rt][mt] = mfma_qk<BF16>(v, __builtin_bit_cast(u32x4, u64x2{pl[rt][0], pl[rt][1]}), acc[rt][mt]);
-                    } else {
-                        acc[rt][mt] = mfma_pv<BF16>(vf[0], ph[rt][0], pl[rt][0], acc[rt][mt]);
+                        acc[rt][mt] = mfma_qk<BF16>(v, u32x4{h[0][0], h[0][1], h[1][0], h[1][1]}, acc[rt][mt]);
+                        acc[rt][mt] = mfma_qk<BF16>(v, u32x4{l[0][0], l[0][1], l[1][0], l[1][1]}, acc[rt][mt]);
+                    } else {        // 16 tokens: both parts in one product, against the same V rows twice
+                        acc[rt][mt] = mfma_qk<BF16>(v, u32x4{h[0][0], h[0][1], l[0][0], l[0][1]}, acc[rt][mt]);
                     }
                 }
             }

@@ -10,6 +10,8 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
+from array import array
 
 import numpy as np
 import torch
@@ -113,18 +115,10 @@ _lib.llmig_decode_attention_migrate.restype = ctypes.c_int
 _lib.llmig_decode_attention_noalloc.argtypes = [_vp, ctypes.c_int32, _vp, ctypes.c_int32, ctypes.c_int32, _vp,
                                                 ctypes.c_int32, _vp, ctypes.c_float, _vp, _vp]
 _lib.llmig_decode_attention_noalloc.restype = ctypes.c_int
+# llmig_append_desc, as the C compiler lays it out
+_append_desc = struct.Struct("@4i4P6q5P3i4x")
 
-
-class _AppendDesc(ctypes.Structure):
-    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("q_heads", ctypes.c_int32),
-                ("table_stride", ctypes.c_int32), ("q", _vp), ("k", _vp), ("v", _vp), ("q_out", _vp),
-                ("q_layer", ctypes.c_int64), ("q_token", ctypes.c_int64), ("k_layer", ctypes.c_int64),
-                ("k_token", ctypes.c_int64), ("v_layer", ctypes.c_int64), ("v_token", ctypes.c_int64),
-                ("tables", _vp), ("from_toks", _vp), ("n_toks", _vp), ("first_pos", _vp), ("cos_sin", _vp),
-                ("positions", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
-
-
-_lib.llmig_append_rotary.argtypes = [_vp, ctypes.POINTER(_AppendDesc), _vp]
+_lib.llmig_append_rotary.argtypes = [_vp, ctypes.c_char_p, _vp]
 _lib.llmig_append_rotary.restype = ctypes.c_int
 _lib.llmig_key_bounds.argtypes = [_vp, _vp, ctypes.c_int32, ctypes.c_int32, _vp, ctypes.c_int32, _vp, _vp, _vp]
 _lib.llmig_key_bounds.restype = ctypes.c_int
@@ -157,8 +151,15 @@ def _check(code: int, where: str) -> None:
         raise LlmigError(code, where)
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int:
     if stream is None:
+        # the handle alone: torch's current_stream() builds an object around
+        # it, 2.4 us of a call's 10
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -537,31 +538,53 @@ def llmig_decode_attention_noalloc(pool: Pool, q: torch.Tensor, tables: torch.Te
     _used_on(stream, q, tables, out)
 
 
-def _dtype_code(t: torch.Tensor, what: str) -> int:
-    if t.dtype not in (torch.float16, torch.bfloat16):
+def _lens(a):
+    """(address, length, keepalive) of host lengths as int32."""
+    if type(a) is list:
+        h = array("i", a)
+        return h.buffer_info()[0], len(h), h
+    h = _host_i32(a)
+    if h.ndim != 1:
+        raise ValueError("lengths must be a list or a vector")
+    return h.ctypes.data, h.size, h
+
+
+_TYPE_CODES = {torch.float16: 0, torch.bfloat16: 1}
+
+
+def _type_code(dtype, what: str) -> int:
+    code = _TYPE_CODES.get(dtype)
+    if code is None:
         raise ValueError(f"{what} must be fp16 or bf16")
-    return 1 if t.dtype == torch.bfloat16 else 0
+    return code
 
 
-def _device_tables(tables: torch.Tensor, batch: int) -> None:
+def _device_tables(tables: torch.Tensor, batch: int) -> int:
+    """Checks block tables; returns their row stride."""
     if tables.dtype != torch.int32 or not tables.is_cuda or not tables.is_contiguous() or tables.dim() != 2:
         raise ValueError("tables must be a contiguous CUDA int32 [batch][stride] tensor")
-    if tables.shape[0] < batch:
+    rows, stride = tables.shape
+    if rows < batch:
         raise ValueError("tables must hold a row per sequence")
+    return stride
 
 
 def _workspace(workspace: torch.Tensor) -> int:
     if not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous CUDA tensor")
-    return workspace.numel() * workspace.element_size()
+    return workspace.nbytes
 
 
-def _row_strides(t: torch.Tensor | None):
-    """Layer and token strides; 0 along an axis of one entry, whose stride in
-    torch may be any number."""
-    if t is None:
-        return 0, 0
-    return tuple(t.stride(i) if t.shape[i] > 1 else 0 for i in (0, 1))
+def _token_rows(t: torch.Tensor, pool: Pool, tokens: int, heads: int, name: str):
+    """Checks [L][tokens][heads][D] rows of new tokens; returns their layer and
+    token strides (0 along an axis of one entry, whose stride may be any)."""
+    layers, dim = pool.num_layers, pool.head_dim
+    if not t.is_cuda or t.dtype != pool.k[0].dtype or t.shape != (layers, tokens, heads, dim):
+        raise ValueError(f"{name} must be a CUDA [layers][tokens][heads][head_dim] tensor of the pool's type")
+    layer, token, head, one = t.stride()
+    if tokens and ((one != 1 and dim > 1) or (head != dim and heads > 1)):
+        raise ValueError(f"the heads of a token of {name} must be contiguous")
+    return layer if layers > 1 else 0, token if tokens > 1 else 0
 
 
 def llmig_append_rotary(pool: Pool, k: torch.Tensor, v: torch.Tensor, tables: torch.Tensor, from_toks, n_toks,
@@ -576,40 +599,36 @@ def llmig_append_rotary(pool: Pool, k: torch.Tensor, v: torch.Tensor, tables: to
     output).  cos_sin: CUDA float32 [positions][rotary_dim], cosines then
     sines (None: no rotation).  first_pos: positions of the first new tokens
     (default: from_toks)."""
-    code, dtype = _dtype_code(k, "k"), pool.k[0].dtype
-    f, n = _host_i32(from_toks), _host_i32(n_toks)
-    if f.ndim != 1 or f.shape != n.shape:
-        raise ValueError("from_toks and n_toks must hold one number per sequence")
-    total, heads = int(n.sum(dtype=np.int64)), pool.num_kv_heads
-    rows = [(k, heads, "k"), (v, heads, "v")]
+    code = _type_code(pool.k[0].dtype, "the pool")
+    fp, batch, f = _lens(from_toks)
+    np_, count, n = _lens(n_toks)
+    pp = p = None
+    if first_pos is not None:
+        pp, places, p = _lens(first_pos)
+    if count != batch or (p is not None and places != batch):
+        raise ValueError("from_toks, n_toks and first_pos must hold one number per sequence")
+    total = sum(n) if type(n) is array else int(n.sum(dtype=np.int64))
+    k_at, v_at = _token_rows(k, pool, total, pool.num_kv_heads, "k"), _token_rows(v, pool, total, pool.num_kv_heads, "v")
+    q_heads, q_at = 0, (0, 0)
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out come together")
     if q is not None:
-        rows.append((q, q.shape[2] if q.dim() == 4 else 0, "q"))
-        if q_out.shape != q.shape or q_out.dtype != dtype or not q_out.is_cuda or not q_out.is_contiguous():
+        if q.dim() != 4:
+            raise ValueError("q must be a [layers][tokens][heads][head_dim] tensor")
+        q_heads = q.shape[2]
+        q_at = _token_rows(q, pool, total, q_heads, "q")
+        if q_out.shape != q.shape or q_out.dtype != q.dtype or not q_out.is_cuda or not q_out.is_contiguous():
             raise ValueError("q_out must be a contiguous CUDA tensor of q's shape and type")
-    for t, h, name in rows:
-        if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != (pool.num_layers, total, h, pool.head_dim):
-            raise ValueError(f"{name} must be a CUDA [layers][tokens][heads][head_dim] tensor of the pool's type")
-        if total and (t.stride(3) != 1 or (h > 1 and t.stride(2) != pool.head_dim)):
-            raise ValueError(f"the heads of a token of {name} must be contiguous")
-    _device_tables(tables, f.size)
-    if cos_sin is not None and (cos_sin.dtype != torch.float32 or not cos_sin.is_cuda or not cos_sin.is_contiguous()
-                                or cos_sin.dim() != 2):
-        raise ValueError("cos_sin must be a contiguous CUDA float32 [positions][rotary_dim] tensor")
-    p = None
-    if first_pos is not None:
-        p = _host_i32(first_pos)
-        if p.shape != f.shape:
-            raise ValueError("first_pos must hold one position per sequence")
-    d = _AppendDesc(code, f.size, q.shape[2] if q is not None else 0, tables.shape[1],
-                    q.data_ptr() if q is not None else None, k.data_ptr(), v.data_ptr(),
-                    q_out.data_ptr() if q is not None else None,
-                    *_row_strides(q), *_row_strides(k), *_row_strides(v), tables.data_ptr(), f.ctypes.data, n.ctypes.data,
-                    p.ctypes.data if p is not None else None, cos_sin.data_ptr() if cos_sin is not None else None,
-                    cos_sin.shape[0] if cos_sin is not None else 0, cos_sin.shape[1] if cos_sin is not None else 0,
-                    1 if interleaved else 0)
-    _check(_lib.llmig_append_rotary(pool.handle, ctypes.byref(d), _stream(stream)), "llmig_append_rotary")
+    stride = _device_tables(tables, batch)
+    positions = rotary = 0
+    if cos_sin is not None:
+        if cos_sin.dtype != torch.float32 or not cos_sin.is_cuda or not cos_sin.is_contiguous() or cos_sin.dim() != 2:
+            raise ValueError("cos_sin must be a contiguous CUDA float32 [positions][rotary_dim] tensor")
+        positions, rotary = cos_sin.shape
+    d = _append_desc.pack(code, batch, q_heads, stride, q.data_ptr() if q_heads else 0, k.data_ptr(), v.data_ptr(),
+                          q_out.data_ptr() if q_heads else 0, *q_at, *k_at, *v_at, tables.data_ptr(), fp, np_, pp or 0,
+                          cos_sin.data_ptr() if rotary else 0, positions, rotary, 1 if interleaved else 0)
+    _check(_lib.llmig_append_rotary(pool.handle, d, _stream(stream)), "llmig_append_rotary")
     _used_on(stream, q, k, v, q_out, tables, cos_sin)
 
 
@@ -618,24 +637,34 @@ def llmig_key_bounds(pool: Pool, bounds: Pool, tables: torch.Tensor, from_toks, 
     ctx_lens[b]) of each sequence were written.  bounds: a pool of block_size
     1 with the cache's layers, blocks, heads, head_dim and type, whose K
     tensors take the least and V tensors the largest key of each block."""
-    code = _dtype_code(pool.k[0], "the pool")
-    if bounds.k[0].dtype != pool.k[0].dtype:
+    dtype = pool.k[0].dtype
+    code = _type_code(dtype, "the pool")
+    if bounds.k[0].dtype != dtype:
         raise ValueError("bounds must be of the pool's type")
-    f, c = _host_i32(from_toks), _host_i32(ctx_lens)
-    if f.ndim != 1 or f.shape != c.shape:
+    fp, batch, f = _lens(from_toks)
+    cp, count, c = _lens(ctx_lens)
+    if count != batch:
         raise ValueError("from_toks and ctx_lens must hold one number per sequence")
-    _device_tables(tables, f.size)
-    _check(_lib.llmig_key_bounds(pool.handle, bounds.handle, code, f.size, tables.data_ptr(), tables.shape[1],
-                                 f.ctypes.data, c.ctypes.data, _stream(stream)), "llmig_key_bounds")
+    stride = _device_tables(tables, batch)
+    _check(_lib.llmig_key_bounds(pool.handle, bounds.handle, code, batch, tables.data_ptr(), stride, fp, cp,
+                                 _stream(stream)), "llmig_key_bounds")
     _used_on(stream, tables)
 
 
 def select_workspace_bytes(bounds: Pool, block_size: int, ctx_lens) -> int:
-    c = _host_i32(ctx_lens)
+    cp, batch, c = _lens(ctx_lens)
     n = ctypes.c_int64(0)
-    _check(_lib.llmig_select_blocks_workspace(bounds.handle, int(block_size), c.ctypes.data, c.size, ctypes.byref(n)),
+    _check(_lib.llmig_select_blocks_workspace(bounds.handle, int(block_size), cp, batch, ctypes.byref(n)),
            "llmig_select_blocks_workspace")
     return n.value
+
+
+def _block_lists(blocks: torch.Tensor, layers: int, batch: int, heads: int) -> int:
+    """Checks lists of blocks; returns their length."""
+    if blocks.dtype != torch.int32 or not blocks.is_cuda or not blocks.is_contiguous() or blocks.dim() != 4 or \
+            blocks.shape[:3] != (layers, batch, heads):
+        raise ValueError("blocks must be a contiguous CUDA int32 [layers][batch][kv_heads][count] tensor")
+    return blocks.shape[3]
 
 
 def llmig_select_blocks(bounds: Pool, block_size: int, q: torch.Tensor, tables: torch.Tensor, ctx_lens,
@@ -644,29 +673,46 @@ def llmig_select_blocks(bounds: Pool, block_size: int, q: torch.Tensor, tables: 
     """Choose blocks for each (layer, sequence, KV head) by what their bounds
     allow a score to reach.  q: CUDA [L][B][Hq][D]; blocks: CUDA int32
     [L][B][kv_heads][count], ascending block numbers, then -1."""
-    code = _dtype_code(q, "q")
-    if not q.is_cuda or not q.is_contiguous() or q.dim() != 4 or q.shape[0] != bounds.num_layers or \
-            q.shape[3] != bounds.head_dim or q.dtype != bounds.k[0].dtype:
+    code = _type_code(q.dtype, "q")
+    if not q.is_cuda or not q.is_contiguous() or q.dim() != 4 or q.dtype != bounds.k[0].dtype:
         raise ValueError("q must be a contiguous CUDA [layers][batch][q_heads][head_dim] tensor of the bounds' type")
-    c = _host_i32(ctx_lens)
-    if c.size != q.shape[1]:
+    layers, batch, q_heads, dim = q.shape
+    if layers != bounds.num_layers or dim != bounds.head_dim:
+        raise ValueError("q must be [layers][batch][q_heads][head_dim] of the bounds' layers and head_dim")
+    cp, count, c = _lens(ctx_lens)
+    if count != batch:
         raise ValueError("ctx_lens must hold one length per sequence of q")
-    _device_tables(tables, c.size)
-    if blocks.dtype != torch.int32 or not blocks.is_cuda or not blocks.is_contiguous() or blocks.dim() != 4 or \
-            tuple(blocks.shape[:3]) != (bounds.num_layers, c.size, bounds.num_kv_heads):
-        raise ValueError("blocks must be a contiguous CUDA int32 [layers][batch][kv_heads][count] tensor")
+    stride = _device_tables(tables, batch)
+    listed = _block_lists(blocks, layers, batch, bounds.num_kv_heads)
     nbytes = _workspace(workspace)
-    _check(_lib.llmig_select_blocks(bounds.handle, code, int(block_size), q.data_ptr(), c.size, q.shape[2],
-                                    tables.data_ptr(), tables.shape[1], c.ctypes.data, int(keep_first),
-                                    int(keep_last), blocks.shape[3], workspace.data_ptr(), nbytes, blocks.data_ptr(),
-                                    _stream(stream)), "llmig_select_blocks")
+    _check(_lib.llmig_select_blocks(bounds.handle, code, int(block_size), q.data_ptr(), batch, q_heads,
+                                    tables.data_ptr(), stride, cp, int(keep_first), int(keep_last), listed,
+                                    workspace.data_ptr(), nbytes, blocks.data_ptr(), _stream(stream)),
+           "llmig_select_blocks")
     _used_on(stream, q, tables, workspace, blocks)
 
 
+def _decode_args(pool: Pool, q: torch.Tensor, tables: torch.Tensor, ctx_lens, out: torch.Tensor):
+    """Checks what the decode attentions share; returns (type code, batch, query
+    heads, table stride, address of the lengths, keepalive)."""
+    code = _type_code(q.dtype, "q")
+    if not q.is_cuda or not q.is_contiguous() or q.dim() != 4 or q.dtype != pool.k[0].dtype:
+        raise ValueError("q must be a contiguous CUDA [layers][batch][q_heads][head_dim] tensor of the pool's type")
+    layers, batch, q_heads, dim = q.shape
+    if layers != pool.num_layers or dim != pool.head_dim:
+        raise ValueError("q must be [layers][batch][q_heads][head_dim] of the pool's layers and head_dim")
+    if out.dtype != torch.float32 or not out.is_cuda or not out.is_contiguous() or out.shape != q.shape:
+        raise ValueError("out must be a contiguous CUDA float32 tensor shaped like q")
+    cp, count, c = _lens(ctx_lens)
+    if count != batch:
+        raise ValueError("ctx_lens must hold one length per sequence of q")
+    return code, batch, q_heads, _device_tables(tables, batch), cp, c
+
+
 def decode_blocks_workspace_bytes(pool: Pool, ctx_lens, q_heads: int, count: int) -> int:
-    c = _host_i32(ctx_lens)
+    cp, batch, c = _lens(ctx_lens)
     n = ctypes.c_int64(0)
-    _check(_lib.llmig_decode_attention_blocks_workspace(pool.handle, c.ctypes.data, c.size, int(q_heads), int(count),
+    _check(_lib.llmig_decode_attention_blocks_workspace(pool.handle, cp, batch, int(q_heads), int(count),
                                                         ctypes.byref(n)), "llmig_decode_attention_blocks_workspace")
     return n.value
 
@@ -675,25 +721,20 @@ def llmig_decode_attention_blocks(pool: Pool, q: torch.Tensor, tables: torch.Ten
                                   scale: float, workspace: torch.Tensor, out: torch.Tensor, stream=None) -> None:
     """llmig_decode_attention of each (layer, sequence, KV head) over the
     blocks that blocks (CUDA int32 [L][B][kv_heads][count]) lists for it."""
-    c = _attention_args(pool, q, tables, ctx_lens, out)
+    code, batch, q_heads, stride, cp, c = _decode_args(pool, q, tables, ctx_lens, out)
+    listed = _block_lists(blocks, pool.num_layers, batch, pool.num_kv_heads)
     nbytes = _workspace(workspace)
-    if blocks.dtype != torch.int32 or not blocks.is_cuda or not blocks.is_contiguous() or blocks.dim() != 4 or \
-            tuple(blocks.shape[:3]) != (pool.num_layers, q.shape[1], pool.num_kv_heads):
-        raise ValueError("blocks must be a contiguous CUDA int32 [layers][batch][kv_heads][count] tensor")
-    _check(_lib.llmig_decode_attention_blocks(pool.handle, 1 if q.dtype == torch.bfloat16 else 0, q.data_ptr(),
-                                              q.shape[1], q.shape[2], tables.data_ptr(), tables.shape[1],
-                                              c.ctypes.data, blocks.data_ptr(), blocks.shape[3], float(scale),
-                                              workspace.data_ptr(), nbytes, out.data_ptr(), _stream(stream)),
-           "llmig_decode_attention_blocks")
+    _check(_lib.llmig_decode_attention_blocks(pool.handle, code, q.data_ptr(), batch, q_heads, tables.data_ptr(), stride,
+                                              cp, blocks.data_ptr(), listed, scale, workspace.data_ptr(), nbytes,
+                                              out.data_ptr(), _stream(stream)), "llmig_decode_attention_blocks")
     _used_on(stream, q, tables, blocks, workspace, out)
 
 
 def decode_prefix_workspace_bytes(pool: Pool, ctx_lens, q_heads: int, prefix_blocks: int) -> int:
-    c = _host_i32(ctx_lens)
+    cp, batch, c = _lens(ctx_lens)
     n = ctypes.c_int64(0)
-    _check(_lib.llmig_decode_attention_prefix_workspace(pool.handle, c.ctypes.data, c.size, int(q_heads),
-                                                        int(prefix_blocks), ctypes.byref(n)),
-           "llmig_decode_attention_prefix_workspace")
+    _check(_lib.llmig_decode_attention_prefix_workspace(pool.handle, cp, batch, int(q_heads), int(prefix_blocks),
+                                                        ctypes.byref(n)), "llmig_decode_attention_prefix_workspace")
     return n.value
 
 
@@ -701,10 +742,9 @@ def llmig_decode_attention_prefix(pool: Pool, q: torch.Tensor, tables: torch.Ten
                                   scale: float, workspace: torch.Tensor, out: torch.Tensor, stream=None) -> None:
     """llmig_decode_attention of a batch whose table rows begin with the same
     prefix_blocks blocks: those are read once for all sequences."""
-    c = _attention_args(pool, q, tables, ctx_lens, out)
+    code, batch, q_heads, stride, cp, c = _decode_args(pool, q, tables, ctx_lens, out)
     nbytes = _workspace(workspace)
-    _check(_lib.llmig_decode_attention_prefix(pool.handle, 1 if q.dtype == torch.bfloat16 else 0, q.data_ptr(),
-                                              q.shape[1], q.shape[2], tables.data_ptr(), tables.shape[1],
-                                              c.ctypes.data, int(prefix_blocks), float(scale), workspace.data_ptr(),
-                                              nbytes, out.data_ptr(), _stream(stream)), "llmig_decode_attention_prefix")
+    _check(_lib.llmig_decode_attention_prefix(pool.handle, code, q.data_ptr(), batch, q_heads, tables.data_ptr(), stride,
+                                              cp, int(prefix_blocks), scale, workspace.data_ptr(), nbytes,
+                                              out.data_ptr(), _stream(stream)), "llmig_decode_attention_prefix")
     _used_on(stream, q, tables, workspace, out)
