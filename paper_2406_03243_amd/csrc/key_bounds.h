@@ -23,53 +23,86 @@ struct BoundsArgs {
     const int32_t *tables;
     uint32_t num_layers, num_blocks, block_size, table_stride, tile_bytes, batch;
     uint32_t slot_chunks;        // 16-byte chunks of a token's keys, and of a block's bounds
+    uint32_t rows;               // rows of lanes that share a block's tokens
+    uint32_t one_each;           // every sequence has one block
     uint32_t first_item;
     Divisor by_slice, by_block;  // by_block: division by the blocks of the call
+    Divisor by_chunk;            // by the chunks of a slice
     uint32_t blocks;             // blocks of the call
     uint32_t block_end[kAppendMaxBatch];  // blocks of the first s + 1 sequences
     int32_t first_block[kAppendMaxBatch]; // first block of sequence s to bring up to date
     int32_t tokens[kAppendMaxBatch];      // tokens of sequence s
 };
 
-// A lane takes 8 dims of one block's keys over its tokens.  A NaN key makes
-// both of its bounds NaN.
+// The less, and the larger; a NaN on either side stays one.
+__device__ __forceinline__ float less_of(float a, float b)
+{
+    return b < a || b != b ? b : a;
+}
+
+__device__ __forceinline__ float larger_of(float a, float b)
+{
+    return b > a || b != b ? b : a;
+}
+
+// A lane takes 8 dims of one block's keys over its row's share of the tokens,
+// eight loads in flight; the rows meet in LDS.  A NaN key makes both of its
+// bounds NaN.
 template <int BF16>
 __global__ void __launch_bounds__(kThreads) key_bounds_rows(const BoundsArgs a)
 {
+    __shared__ u32x4 part[2][kThreads];
     const uint32_t item = a.first_item + blockIdx.x;
     const uint32_t unit = divide(item, a.by_slice), slice = item - unit * a.by_slice.d;
     const uint32_t layer = divide(unit, a.by_block), i = unit - layer * a.blocks;
-    uint32_t s = 0, hi = a.batch - 1;
-    while (s < hi) {
-        const uint32_t mid = (s + hi) / 2u;
-        if (a.block_end[mid] <= i)
-            s = mid + 1u;
-        else
-            hi = mid;
-    }
+    const uint32_t s = a.one_each ? i : sequence_of(a.block_end, a.batch, i);
     const uint32_t blk = static_cast<uint32_t>(a.first_block[s]) + i - (s > 0 ? a.block_end[s - 1] : 0u);
     const uint32_t id = table_id(a.tables, s, a.table_stride, blk);
     const uint32_t held = min(static_cast<uint32_t>(a.tokens[s]) - blk * a.block_size, a.block_size);
-    const uint32_t chunk = slice * kThreads + threadIdx.x;
-    if (chunk >= a.slot_chunks || id >= a.num_blocks)
+    if (id >= a.num_blocks)
         return;
+    const uint32_t r = divide(threadIdx.x, a.by_chunk), mine = threadIdx.x - r * a.by_chunk.d;
+    const uint32_t chunk = slice * kThreads + mine;
+    const bool in = r < a.rows && chunk < a.slot_chunks;
     const uint8_t *row = reinterpret_cast<const uint8_t *>(table_entry(a.tab, layer)) +
-                         static_cast<uint64_t>(id) * a.tile_bytes + chunk * 16u;
+                         static_cast<uint64_t>(id) * a.tile_bytes + (in ? chunk : 0u) * 16u;
     float lo[8], up[8];
-    unpack8<BF16>(load16(row), lo);
+    for (uint32_t t = in ? r : 0u, first = 1; t < held || first; t += 8u * a.rows) {
+        u32x4 x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        up[e] = lo[e];
-#pragma unroll 8
-    for (uint32_t t = 1; t < held; ++t) {
-        float x[8];
-        unpack8<BF16>(load16(row + static_cast<uint64_t>(t) * a.slot_chunks * 16u), x);
+        for (uint32_t u = 0; u < 8; ++u)       // (a token twice changes nothing)
+            x[u] = load16(row + static_cast<uint64_t>(min(t + u * a.rows, held - 1u)) * a.slot_chunks * 16u);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            lo[e] = x[e] < lo[e] || x[e] != x[e] ? x[e] : lo[e];
-            up[e] = x[e] > up[e] || x[e] != x[e] ? x[e] : up[e];
+        for (uint32_t u = 0; u < 8; ++u) {
+            float f[8];
+            unpack8<BF16>(x[u], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                lo[e] = u == 0 && first ? f[e] : less_of(lo[e], f[e]);
+                up[e] = u == 0 && first ? f[e] : larger_of(up[e], f[e]);
+            }
+        }
+        first = 0;
+    }
+    if (a.rows > 1) {
+        part[0][threadIdx.x] = pack8<BF16>(lo);
+        part[1][threadIdx.x] = pack8<BF16>(up);
+        __syncthreads();
+        if (r > 0)
+            return;
+        for (uint32_t k = 1; k < a.rows; ++k) {
+            float f[8], h[8];
+            unpack8<BF16>(part[0][k * a.by_chunk.d + mine], f);
+            unpack8<BF16>(part[1][k * a.by_chunk.d + mine], h);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                lo[e] = less_of(lo[e], f[e]);
+                up[e] = larger_of(up[e], h[e]);
+            }
         }
     }
+    if (!in)
+        return;
     const uint64_t at = (static_cast<uint64_t>(id) * a.slot_chunks + chunk) * 16u;
     *(LLMIG_GLOBAL u32x4 *)(table_entry(a.bounds_tab, layer) + at) = pack8<BF16>(lo);
     *(LLMIG_GLOBAL u32x4 *)(table_entry(a.bounds_tab, a.num_layers + layer) + at) = pack8<BF16>(up);

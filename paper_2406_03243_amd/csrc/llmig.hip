@@ -1522,17 +1522,19 @@ int llmig_append_rotary(const llmig_pool *pool, const llmig_append_desc *d, void
     const int64_t L = pool->num_layers, bs = pool->block_size, D = pool->head_dim;
     AppendArgs a;
     std::memset(&a, 0, sizeof(a));
-    int64_t n = 0;
+    int64_t n = 0, most = 0;
     for (int32_t b = 0; b < d->batch; ++b) {
         const int64_t from = d->from_toks[b], add = d->n_toks[b], pos = d->first_pos ? d->first_pos[b] : from;
         if (from < 0 || add < 0 || pos < 0 || from + add > 0x7fffffffLL)
             return LLMIG_EINVAL;
         if (add > 0 && ((from + add - 1) / bs >= d->table_stride || (d->rotary_dim > 0 && pos + add > d->positions)))
             return LLMIG_EINVAL;
+        a.token_first[b] = static_cast<uint32_t>(n);
         n += add;
         if (n > 0x7fffffffLL / L)
             return LLMIG_EINVAL;
-        a.token_end[b] = static_cast<uint32_t>(n);
+        most = std::max(most, add);
+        a.one_each = b == 0 ? add == 1 : a.one_each && add == 1;
         a.from[b] = d->from_toks[b];
         a.pos[b] = static_cast<int32_t>(pos);
     }
@@ -1576,21 +1578,78 @@ int llmig_append_rotary(const llmig_pool *pool, const llmig_append_desc *d, void
     a.tokens = static_cast<uint32_t>(n);
     a.batch = static_cast<uint32_t>(d->batch);
     a.row_chunks = static_cast<uint32_t>(D / 8);
-    a.token_chunks = (a.q_heads + 2u * a.kv_heads) * a.row_chunks;
     a.half = static_cast<uint32_t>(d->rotary_dim / 2);
     a.interleaved = static_cast<uint32_t>(d->interleaved);
     a.wide = a.half % 4 == 0 && (reinterpret_cast<uintptr_t>(d->cos_sin) & 15u) == 0;
     a.layouts[0] = pool->layouts[0];
     a.layouts[1] = pool->layouts[1];
-    const uint32_t slices = (a.token_chunks + kThreads - 1) / kThreads;
-    a.by_slice = divisor(slices);
-    a.by_layer = divisor(a.num_layers);
-    a.by_row = divisor(a.row_chunks);
     a.by_block = divisor(a.block_size);
-    const void *fn = d->dtype ? reinterpret_cast<const void *>(&append_rotary_rows<1>)
-                              : reinterpret_cast<const void *>(&append_rotary_rows<0>);
-    return launch_items(fn, &a, static_cast<uint64_t>(n) * L * slices, slices, &a.first_unit,
-                        static_cast<hipStream_t>(stream));
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    // tensors that go block by block: several tokens of a sequence, into a
+    // layout whose tokens' rows do not lie in one piece
+    bool by_blocks[2];
+    for (int k = 0; k < 2; ++k)
+        by_blocks[k] = most >= kAppendBlockTokens && (pool->layouts[k] == LLMIG_LAYOUT_HCNX ||
+                                                      (pool->layouts[k] == LLMIG_LAYOUT_HDN && bs % 8 == 0 && bs / 8 <= kThreads));
+    a.rows_heads[0] = a.q_heads;
+    a.rows_heads[1] = by_blocks[0] ? 0 : a.kv_heads;
+    a.rows_heads[2] = by_blocks[1] ? 0 : a.kv_heads;
+    const uint32_t rows_heads = a.rows_heads[0] + a.rows_heads[1] + a.rows_heads[2];
+    const uint32_t pairs = (a.row_chunks + 1) / 2;
+    const bool fast = a.half % 8 == 0 && a.wide;
+    // launches `units` tokens or blocks whose lanes move pairs of chunks
+    auto launch_pairs = [&](uint64_t units, bool slots) {
+        const uint32_t slices = (a.lanes + kThreads - 1) / kThreads;
+        const uint32_t layers = fast ? append_layers(units * L * slices) : 1;
+        const uint32_t groups = (a.num_layers + layers - 1) / layers;
+        a.by_slice = divisor(slices);
+        a.by_layer = divisor(groups);
+        a.by_row = divisor(pairs);
+        return launch_items(d->dtype ? append_kernel<1>(slots, layers, fast) : append_kernel<0>(slots, layers, fast), &a, units * groups * slices, slices,
+                            &a.first_unit, st);
+    };
+    if (rows_heads > 0) {
+        a.lanes = rows_heads * pairs;
+        for (int32_t b = 0; b < d->batch; ++b)
+            a.unit_end[b] = b + 1 < d->batch ? a.token_first[b + 1] : a.tokens;
+        const int rc = launch_pairs(static_cast<uint64_t>(n), false);
+        if (rc != LLMIG_OK)
+            return rc;
+    }
+    if (!by_blocks[0] && !by_blocks[1])
+        return LLMIG_OK;
+    int64_t blocks = 0;
+    for (int32_t b = 0; b < d->batch; ++b) {
+        if (d->n_toks[b] > 0)
+            blocks += (static_cast<int64_t>(d->from_toks[b]) + d->n_toks[b] - 1) / bs - d->from_toks[b] / bs + 1;
+        a.unit_end[b] = static_cast<uint32_t>(blocks);
+    }
+    for (uint32_t k = 0; k < 2; ++k) {
+        if (!by_blocks[k])
+            continue;
+        a.tensor = k;
+        int rc;
+        if (pool->layouts[k] == LLMIG_LAYOUT_HCNX) {
+            a.lanes = a.kv_heads * pairs * a.block_size;
+            a.by_group = divisor(bs % 8 == 0 ? 8 : a.block_size);
+            a.by_groups = divisor(a.block_size / a.by_group.d);
+            rc = launch_pairs(static_cast<uint64_t>(blocks), true);
+        } else {
+            const uint32_t along = a.block_size / 8;
+            a.lanes = a.kv_heads * a.row_chunks * along;
+            const uint32_t chunks = a.lanes <= static_cast<uint32_t>(kThreads) ? a.lanes / along : kThreads / along;
+            const uint32_t slices = (a.kv_heads * a.row_chunks + chunks - 1) / chunks;
+            a.by_slice = divisor(slices);
+            a.by_layer = divisor(a.num_layers);
+            a.by_row = divisor(along);
+            rc = launch_items(d->dtype ? reinterpret_cast<const void *>(&append_rotary_dims<1>)
+                                       : reinterpret_cast<const void *>(&append_rotary_dims<0>),
+                              &a, static_cast<uint64_t>(blocks) * L * slices, slices, &a.first_unit, st);
+        }
+        if (rc != LLMIG_OK)
+            return rc;
+    }
+    return LLMIG_OK;
 }
 
 int llmig_key_bounds(const llmig_pool *pool, const llmig_pool *bounds, int32_t dtype, int32_t batch,
@@ -1612,8 +1671,10 @@ int llmig_key_bounds(const llmig_pool *pool, const llmig_pool *bounds, int32_t d
             return LLMIG_EINVAL;
         a.first_block[b] = from_toks[b] / pool->block_size;
         a.tokens[b] = ctx_lens[b];
+        const int64_t before = n;
         if (from_toks[b] < ctx_lens[b])
             n += blocks_of(ctx_lens[b], pool->block_size) - a.first_block[b];
+        a.one_each = (b == 0 || a.one_each) && n - before == 1;
         a.block_end[b] = static_cast<uint32_t>(n);
     }
     a.slot_chunks = static_cast<uint32_t>(pool->num_kv_heads * (pool->head_dim / 8));
@@ -1632,8 +1693,11 @@ int llmig_key_bounds(const llmig_pool *pool, const llmig_pool *bounds, int32_t d
     a.tile_bytes = static_cast<uint32_t>(pool->tile_bytes);
     a.batch = static_cast<uint32_t>(batch);
     a.blocks = static_cast<uint32_t>(n);
+    const uint32_t chunks = std::min(a.slot_chunks, static_cast<uint32_t>(kThreads));
+    a.rows = std::min(kThreads / chunks, a.block_size);
     a.by_slice = divisor(slices);
     a.by_block = divisor(a.blocks);
+    a.by_chunk = divisor(chunks);
     const void *fn = dtype ? reinterpret_cast<const void *>(&key_bounds_rows<1>)
                            : reinterpret_cast<const void *>(&key_bounds_rows<0>);
     return launch_items(fn, &a, static_cast<uint64_t>(n) * pool->num_layers * slices, 1, &a.first_item,
