@@ -1939,10 +1939,9 @@ int llmig_decode_attention_prefix(const llmig_pool *pool, int32_t dtype, const v
         j.seq[s] = r.seq[s];
         j.member[s] = place[r.seq[s]];
     }
-    const void *jfn = pool->head_dim == 64 ? reinterpret_cast<const void *>(&prefix_join<64>)
-                                           : reinterpret_cast<const void *>(&prefix_join<128>);
-    const uint64_t per = kThreads / (pool->head_dim / 4);
-    for (uint64_t at = 0; at < rows; at += kMaxGridWorkgroups * per) {
+    uint32_t per = 0;
+    const void *jfn = prefix_join_kernel(pool->head_dim, most + p.cut.parts, &per);
+    for (uint64_t at = 0; at < rows; at += static_cast<uint64_t>(kMaxGridWorkgroups) * per) {
         j.row_base = static_cast<uint32_t>(at);
         void *jargs[] = {&j};
         e = hipLaunchKernel(jfn, dim3(static_cast<uint32_t>(std::min<uint64_t>((rows - at + per - 1) / per, kMaxGridWorkgroups))),

@@ -337,58 +337,80 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
 }
 
 // Joins the records of the prefix and of a sequence's own tokens.  D / 4 lanes
-// a row (layer, sequence, query head), eight records' loads in flight.
-template <int D>
+// a row (layer, sequence, query head) and record, SUB of them side by side, each
+// with every SUB-th record, eight records' loads in flight; they meet in LDS.
+template <int D, int SUB>
 __global__ void __launch_bounds__(kThreads) prefix_join(const PrefixJoinArgs a)
 {
-    constexpr uint32_t kQuads = D / 4, kRec = D + kAttnHeader;
-    const uint32_t d4 = threadIdx.x % kQuads;
-    const uint32_t r = a.row_base + blockIdx.x * (kThreads / kQuads) + threadIdx.x / kQuads;
+    constexpr uint32_t kQuads = D / 4, kRec = D + kAttnHeader, kRows = kThreads / (kQuads * SUB);
+    const uint32_t d4 = threadIdx.x % kQuads, sub = threadIdx.x / kQuads % SUB, mine = threadIdx.x / (kQuads * SUB);
     const uint32_t rows = a.num_layers * a.batch * a.q_heads;
-    if (r >= rows)
-        return;
+    const uint32_t r0 = a.row_base + blockIdx.x * kRows + mine;
+    const uint32_t r = min(r0, rows - 1u);
     const uint32_t h = r % a.q_heads, s = r / a.q_heads % a.batch, layer = r / a.q_heads / a.batch;
     const uint32_t first = s > 0 ? a.seq_end[s - 1] : 0u;
-    const uint32_t own = a.seq_end[s] - first;
-    const uint32_t shared = a.member[s] < a.members ? a.parts : 0u;
-    const float *pre = a.prefix + ((static_cast<uint64_t>(layer) * a.parts * a.members + a.member[s]) * a.q_heads + h) * kRec;
-    const float *mine = a.own + ((static_cast<uint64_t>(layer) * a.n_records + first) * a.q_heads + h) * kRec;
+    const uint32_t place = a.member[s], shared = place < a.members ? a.parts : 0u;
+    const uint32_t all = shared + a.seq_end[s] - first;
+    const float *pre = a.prefix + ((static_cast<uint64_t>(layer) * a.parts * a.members + place) * a.q_heads + h) * kRec;
+    const float *own = a.own + ((static_cast<uint64_t>(layer) * a.n_records + first) * a.q_heads + h) * kRec;
     const uint64_t pre_step = static_cast<uint64_t>(a.members) * a.q_heads * kRec;
     const uint64_t own_step = static_cast<uint64_t>(a.q_heads) * kRec;
     float m = -INFINITY, l = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (uint32_t p0 = 0; p0 < shared + own; p0 += 8) {
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](float m2, float l2, f32x4_t v) {
+        const float mm = fmaxf(m, m2);
+        if (mm == -INFINITY) {      // no weight on either side; a NaN sum stays one
+            l += l2;
+            return;
+        }
+        const float c1 = __expf(m - mm), c2 = __expf(m2 - mm);
+        l = l * c1 + l2 * c2;
+        acc = acc * c1 + v * c2;
+        m = mm;
+    };
+    for (uint32_t p0 = sub; p0 < all; p0 += 8 * SUB) {
         float2 ml[8];
-        float4 v[8];
+        f32x4_t v[8];
 #pragma unroll
         for (uint32_t u = 0; u < 8; ++u) {
-            const uint32_t p = p0 + u;
+            const uint32_t p = p0 + u * SUB;
             ml[u] = make_float2(-INFINITY, 0.f);
-            v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (p < shared + own) {
-                const float *src = p < shared ? pre + p * pre_step : mine + (p - shared) * own_step;
+            v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            if (p < all) {
+                const float *src = p < shared ? pre + p * pre_step : own + (p - shared) * own_step;
                 ml[u] = *reinterpret_cast<const float2 *>(src);
-                v[u] = *reinterpret_cast<const float4 *>(src + kAttnHeader + 4 * d4);
+                v[u] = *reinterpret_cast<const f32x4_t *>(src + kAttnHeader + 4 * d4);
             }
         }
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const float mm = fmaxf(m, ml[u].x);
-            if (mm == -INFINITY) {      // no weight on either side; a NaN sum stays one
-                l += ml[u].y;
-                continue;
-            }
-            const float c1 = __expf(m - mm), c2 = __expf(ml[u].x - mm);
-            l = l * c1 + ml[u].y * c2;
-            acc.x = acc.x * c1 + v[u].x * c2;
-            acc.y = acc.y * c1 + v[u].y * c2;
-            acc.z = acc.z * c1 + v[u].z * c2;
-            acc.w = acc.w * c1 + v[u].w * c2;
-            m = mm;
-        }
+        for (int u = 0; u < 8; ++u)
+            add(ml[u].x, ml[u].y, v[u]);
     }
-    reinterpret_cast<float4 *>(a.out)[((static_cast<uint64_t>(layer) * a.batch + a.seq[s]) * a.q_heads + h) * kQuads + d4] =
-        l > 0.f ? make_float4(acc.x / l, acc.y / l, acc.z / l, acc.w / l) : make_float4(0.f, 0.f, 0.f, 0.f);
+    if constexpr (SUB > 1) {
+        __shared__ float2 sh_ml[kRows][SUB];
+        __shared__ f32x4_t sh_v[kRows][SUB][kQuads];
+        sh_v[mine][sub][d4] = acc;
+        if (d4 == 0)
+            sh_ml[mine][sub] = make_float2(m, l);
+        __syncthreads();
+        if (sub > 0)
+            return;
+#pragma unroll
+        for (int u = 1; u < SUB; ++u)
+            add(sh_ml[mine][u].x, sh_ml[mine][u].y, sh_v[mine][u][d4]);
+    }
+    if (r0 < rows)
+        reinterpret_cast<f32x4_t *>(a.out)[((static_cast<uint64_t>(layer) * a.batch + a.seq[s]) * a.q_heads + h) * kQuads + d4] =
+            l > 0.f ? acc / l : f32x4_t{0.f, 0.f, 0.f, 0.f};
+}
+
+// The join for at most `most` records a row; its rows per workgroup.
+inline const void *prefix_join_kernel(int head_dim, uint32_t most, uint32_t *rows)
+{
+    *rows = kThreads / (head_dim / 4) / (most <= 8 ? 1u : 8u);
+    if (head_dim == 64)
+        return most <= 8 ? reinterpret_cast<const void *>(&prefix_join<64, 1>) : reinterpret_cast<const void *>(&prefix_join<64, 8>);
+    return most <= 8 ? reinterpret_cast<const void *>(&prefix_join<128, 1>) : reinterpret_cast<const void *>(&prefix_join<128, 8>);
 }
 
 template <int BF16, int D>
