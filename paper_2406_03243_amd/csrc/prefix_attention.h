@@ -14,9 +14,11 @@
 #include "append_rotary.h"
 #include "decode_attention.h"
 
+#include <type_traits>
+
 namespace {
 
-constexpr uint32_t kPrefixTile = 64;      // tokens of K and V in LDS at a time
+constexpr uint32_t kPrefixTile = 128;     // tokens of K and V in LDS at a time
 
 struct PrefixArgs {
     const uint64_t *tab;         // pool table: K bases then V bases
@@ -43,22 +45,30 @@ struct PrefixJoinArgs {
     uint8_t seq[kAttnMaxBatch];           // its number in the batch
 };
 
-// x of the lane 16, or 32, lanes away (in either direction of its row pair,
-// half pair): the larger, and the sum.
-__device__ __forceinline__ float max_of_rows(float x)
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+template <int BF16>
+__device__ __forceinline__ f32x16_t mfma_32(u32x4 a, u32x4 b, f32x16_t c)
 {
-    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    if constexpr (BF16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
+                                                       0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c,
+                                                      0, 0, 0);
 }
 
-__device__ __forceinline__ float sum_of_rows(float x)
+// The larger, and the sum, of x of lanes l and l + 32, in both.
+__device__ __forceinline__ float max_of_halves(float x)
 {
-    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+__device__ __forceinline__ float sum_of_halves(float x)
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
 // Two weights as their 16-bit roundings and the 16-bit roundings of what these
@@ -82,25 +92,27 @@ __device__ __forceinline__ void split_weights(float p0, float p1, uint32_t *hi, 
     }
 }
 
+// The rows of 16 tokens of a block: a multiple of 16 tokens a block (ALIGNED)
+// puts each such group in one, so its row is found with scalar instructions.
+//
 // One workgroup: a partition of one (layer, KV head) against 32 * WM query
-// rows.  Of its four wavefronts WM split the rows, 32 each (two MFMA columns
-// of 16), and 4 / WM the tokens of each tile.
-template <int BF16, int D, int WM>
+// rows.  Of its four wavefronts WM split the rows, 32 each (the columns of one
+// MFMA), and 4 / WM the tokens of each tile.
+template <int BF16, int D, int WM, int ALIGNED>
 __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
 {
-    constexpr int KS = D / 32;                     // k-steps of the QK product
-    constexpr int MT = D / 16;                     // 16-dim tiles of the PV product
-    constexpr int LPR = D / 8;                     // 16-byte chunks of a row
-    constexpr int RB = D * 2;                      // bytes of a row
-    constexpr int RPB = 128 / D;                   // rows per 256 bytes
-    constexpr int TT = kPrefixTile / 16 * WM / 4;  // 16-token groups of a tile per wavefront
-    constexpr int STEP = TT > 1 ? 2 : 1;           // groups taken at a time
-    constexpr int CPT = kPrefixTile * LPR / kThreads;   // chunks of K, and of V, a thread brings per tile
+    constexpr int KS = D / 16;                     // k-steps of the QK product
+    constexpr int MT = D / 32;                     // 32-dim tiles of the PV product
+    constexpr uint32_t LPR = D / 8;                // 16-byte chunks of a row
+    constexpr uint32_t RB = D * 2;                 // bytes of a row
+    constexpr uint32_t RPB = 128 / D;              // rows per 256 bytes
+    constexpr int CPT = kPrefixTile * LPR / kThreads;    // chunks of K, and of V, a thread brings per tile
+    constexpr uint32_t RPI = kThreads / LPR;       // rows that the threads bring at a time
     constexpr float kLog2e = 1.4426950408889634f;
-    constexpr int kTileBytes = kPrefixTile * RB;
-    constexpr int kMergeRow = D + 4;
-    __shared__ __align__(16) uint8_t smem[2][2][kTileBytes];      // buffer, K or V
-    static_assert(4 * 16 * kMergeRow * 4 <= 4 * kTileBytes, "the merge of 16 rows fits");
+    constexpr uint32_t kTileBytes = kPrefixTile * RB;
+    constexpr uint32_t kMergeRow = D + 4;
+    __shared__ __align__(16) uint8_t smem[2][kTileBytes];         // K, V
+    static_assert(4 * 16 * kMergeRow * 4 <= 2 * kTileBytes, "the merge of 16 rows fits");
     __shared__ float sh_m[4][32], sh_l[4][32];
 
     // The workgroups that read the same tokens (a partition's row chunks, then
@@ -120,192 +132,218 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
     const uint32_t t_begin = part * a.part_tokens, t_end = min(t_begin + a.part_tokens, a.tokens);
     const uint32_t wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64;
     const uint32_t wm = wave % WM, wt = wave / WM;
-    const uint32_t r16 = lane % 16, g4 = lane / 16;
+    const uint32_t l32 = lane % 32, half = lane / 32;
     const uint32_t G = a.q_heads / a.kv_heads, M = a.members * G;
     const uint8_t *kbase = reinterpret_cast<const uint8_t *>(table_entry(a.tab, layer));
     const uint8_t *vbase = reinterpret_cast<const uint8_t *>(table_entry(a.tab, a.num_layers + layer));
 
-    // Q^T fragments (B operand): dims 32 * ks + 8 * g4 .. + 8 of the lane's row
-    // of each column block; rows past the last: the last again, stored nowhere.
-    const uint32_t row0 = chunk * 32u * WM + wm * 32u;
-    u32x4 qf[2][KS];
-#pragma unroll
-    for (int rt = 0; rt < 2; ++rt) {
-        const uint32_t r = min(row0 + 16u * rt + r16, M - 1u);
+    // Q^T fragments (B operand): dims 16 * ks + 8 * half .. + 8 of the lane's row;
+    // rows past the last: the last again, stored nowhere.  A negative scale turns
+    // the queries' signs, so that scores rise with their products.
+    u32x4 qf[KS];
+    {
+        const uint32_t r = min(chunk * 32u * WM + wm * 32u + l32, M - 1u);
         const uint64_t q_row = (static_cast<uint64_t>(layer) * a.batch + a.member[r / G]) * a.q_heads + g * G + r % G;
+        const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            // a negative scale: the queries' signs turn, so that scores rise
-            // with their products
-            qf[rt][ks] = load16(a.q + (q_row * D + 32 * ks + 8 * g4) * 2) ^ (a.scale < 0.f ? 0x80008000u : 0u);
-        }
+        for (int ks = 0; ks < KS; ++ks)
+            qf[ks] = load16(a.q + (q_row * D + 16 * ks + 8 * half) * 2) ^ sign;
     }
 
-    // A tile's rows: thread's chunk of token th + i * (kThreads / LPR), brought
-    // into registers while the tile before it is worked on, and their blocks'
-    // ids one tile ahead of them.  Tokens past the partition's end repeat its
-    // last one; they weigh 0.
+    // A tile's rows: the thread's chunk of token th + i * RPI, brought into
+    // registers while the tile before it is worked on, and their blocks' ids one
+    // tile ahead of them.  Past the partition's end valid rows repeat; they
+    // weigh 0.
     const uint32_t th = threadIdx.x / LPR, tc = threadIdx.x % LPR;
     u32x4 kr[CPT], vr[CPT];
     uint32_t ids[CPT];
-    auto token_of = [&](uint32_t t0, int i) { return min(t0 + th + i * (kThreads / LPR), t_end - 1u); };
+    // ALIGNED: the first of the 16 tokens (t_end is a multiple of 16) to which the
+    // wavefront's rows of load i belong; else the thread's token.
+    const uint32_t wave_row = wave * (64u / LPR);
+    auto token_of = [&](uint32_t t0, uint32_t i) {
+        return ALIGNED ? min(t0 + (i * RPI + wave_row) / 16u * 16u, t_end - 16u) : min(t0 + i * RPI + th, t_end - 1u);
+    };
+    const uint64_t lane_at = (ALIGNED ? static_cast<uint64_t>(th % 16u) * a.kv_heads * RB : 0u) + 16u * tc;
     auto look_up = [&](uint32_t t0) {
 #pragma unroll
-        for (int i = 0; i < CPT; ++i)
-            ids[i] = static_cast<uint32_t>(a.table[divide(token_of(t0, i), a.by_block)]);
+        for (int i = 0; i < CPT; ++i) {
+            const uint32_t blk = divide(token_of(t0, i), a.by_block);
+            ids[i] = ALIGNED ? static_cast<uint32_t>(id_entry(a.table, uniform(blk))) : static_cast<uint32_t>(a.table[blk]);
+        }
     };
     auto fetch = [&](uint32_t t0) {
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
             const uint32_t t = token_of(t0, i), blk = divide(t, a.by_block);
             const uint64_t slot = static_cast<uint64_t>(min(ids[i], a.num_blocks - 1u)) * a.block_size + (t - blk * a.block_size);
-            const uint64_t at = (slot * a.kv_heads + g) * RB + 16u * tc;
+            const uint64_t at = (slot * a.kv_heads + g) * RB + lane_at;
             kr[i] = *(const LLMIG_GLOBAL u32x4 *)(kbase + at);
             vr[i] = *(const LLMIG_GLOBAL u32x4 *)(vbase + at);
         }
     };
-    // 16-byte chunk c of token t sits at chunk c ^ swz(t) of its row, so that
-    // reads of 16 rows at once fall on distinct banks.
-    auto swz = [](uint32_t t) { return (t / RPB) % LPR; };
-    auto put = [&](uint32_t buf) {
+    // 16-byte chunk c of token t sits at chunk c ^ swizzle(t) of its row, so that
+    // what is read at once falls on distinct banks: of K a chunk of each of 16
+    // rows, of V four chunks of each of 4 rows.
+    auto k_swizzle = [](uint32_t t) { return (t / RPB) % LPR; };
+    auto v_swizzle = [](uint32_t t) { return t / RPB % (4u / RPB) * 4u ^ t / 4u % 4u; };
+    static_assert(RPI % 16 == 0, "a thread's rows swizzle alike");
+    const uint32_t put_k = th * RB + 16u * (tc ^ k_swizzle(th)), put_v = th * RB + 16u * (tc ^ v_swizzle(th));
+    auto put = [&]() {
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
-            const uint32_t t = th + i * (kThreads / LPR), at = t * RB + 16u * (tc ^ swz(t));
-            *reinterpret_cast<u32x4 *>(&smem[buf][0][at]) = kr[i];
-            *reinterpret_cast<u32x4 *>(&smem[buf][1][at]) = vr[i];
+            *reinterpret_cast<u32x4 *>(&smem[0][put_k + i * RPI * RB]) = kr[i];
+            *reinterpret_cast<u32x4 *>(&smem[1][put_v + i * RPI * RB]) = vr[i];
         }
     };
 
+    // Operands out of LDS.  K (A operand): token l32, dims 16 * ks + 8 * half .. + 8.
+    // V^T (A operand: dim 32 * mt + l32) by transposing reads: lane r16 of a
+    // 16-lane group receives element r16 % 4 of the 8 bytes that lane 4 * q +
+    // r16 / 4 of its group addresses, for q = 0..3: tokens 4 * half + q of 8.
+    const uint32_t r16 = lane % 16;
+    const uint32_t k_at = l32 * RB, k_x = 16u * (half ^ k_swizzle(l32));
+    const uint32_t v_row = 4u * half + r16 / 4u;
+    const uint32_t v_at = v_row * RB + 8u * (r16 % 2u), v_x = 16u * ((2u * (lane / 16u % 2u) + r16 % 4u / 2u) ^ v_swizzle(v_row));
+
     const float qk_scale = fabsf(a.scale) * kLog2e;
-    float m[2] = {-INFINITY, -INFINITY}, lsum[2] = {0.f, 0.f};
-    f32x4_t acc[2][MT];
+    float m = -INFINITY, lsum = 0.f;
+    f32x16_t acc[MT];
 #pragma unroll
-    for (int rt = 0; rt < 2; ++rt)
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-            acc[rt][mt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < 16; ++i)
+            acc[mt][i] = 0.f;
+
+    // A tile in LDS; TAIL: the partition ends in it.
+    auto work = [&](uint32_t t0, auto tail_c) {
+        constexpr bool TAIL = decltype(tail_c)::value;
+        const uint8_t *kt = smem[0] + wt * (32u * WM) * RB, *vt = smem[1] + wt * (32u * WM) * RB;
+        // S^T = K . Q^T of 32 tokens
+        auto scores = [&](int step) {
+            f32x16_t s;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                s[i] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const u32x4 kf = *reinterpret_cast<const u32x4 *>(kt + 32 * step * RB + k_at + (k_x ^ (32u * ks)));
+                s = mfma_32<BF16>(kf, qf[ks], s);
+            }
+            return s;
+        };
+        f32x16_t s = scores(0);
+#pragma unroll
+        for (int step = 0; step < WM; ++step) {
+            // element i of s is token first + 8 * (i / 4) + i % 4, of query row l32
+            const uint32_t first = t0 + 32u * (wt * WM + step) + 4u * half;
+            if constexpr (TAIL) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    s[i] = first + 8u * (i / 4) + i % 4 < t_end ? s[i] : -INFINITY;
+            }
+            // The maximum that weights are taken against moves only when a score
+            // exceeds it by 2^8: the sums have the room, and the accumulators are
+            // rescaled seldom.
+            float mx = s[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i)
+                mx = fmaxf(mx, s[i]);
+            mx *= qk_scale;
+            if (__ballot(mx > m + 8.f)) {
+                const float m_new = fmaxf(m, max_of_halves(mx));
+                const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+                lsum *= c;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    acc[mt] = acc[mt] * c;
+                m = m_new;
+            }
+            f32x16_t s_next;
+            if (step + 1 < WM)
+                s_next = scores(step + 1);
+            const float m_sub = m == -INFINITY ? 0.f : m;
+            float p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                p[i] = __builtin_amdgcn_exp2f(s[i] * qk_scale - m_sub);
+            if constexpr (TAIL) {       // (a scale of 0 would make NaN of the mask's -inf)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    p[i] = first + 8u * (i / 4) + i % 4 < t_end ? p[i] : 0.f;
+            }
+            uint32_t hi[8], lo[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                lsum += p[2 * i] + p[2 * i + 1];
+                split_weights<BF16>(p[2 * i], p[2 * i + 1], &hi[i], &lo[i]);
+            }
+            // O^T += V^T . P^T, 16 tokens at a time, the weights as their 16-bit
+            // rounding and the 16-bit rounding of the rest
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                u32x4 vf[MT];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    uint64_t v[2];
+#pragma unroll
+                    for (uint32_t j = 0; j < 2; ++j)
+                        v[j] = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                            (LLMIG_LDS i16x4_t *)(vt + (32 * step + 16 * n + 8 * j) * RB + v_at +
+                                                  (v_x ^ (64u * mt) ^ (32u * j)))));
+                    typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+                    vf[mt] = __builtin_bit_cast(u32x4, u64x2{v[0], v[1]});
+                }
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    acc[mt] = mfma_32<BF16>(vf[mt], u32x4{hi[4 * n], hi[4 * n + 1], hi[4 * n + 2], hi[4 * n + 3]}, acc[mt]);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    acc[mt] = mfma_32<BF16>(vf[mt], u32x4{lo[4 * n], lo[4 * n + 1], lo[4 * n + 2], lo[4 * n + 3]}, acc[mt]);
+            }
+            if (step + 1 < WM)
+                s = s_next;
+        }
+    };
 
     look_up(t_begin);
     fetch(t_begin);
     look_up(t_begin + kPrefixTile);
-    put(0);
-    uint32_t buf = 0;
-    for (uint32_t t0 = t_begin; t0 < t_end; t0 += kPrefixTile, buf ^= 1u) {
-        __syncthreads();                      // the tile is in LDS, and the one before it is done with
-        const bool more = t0 + kPrefixTile < t_end;
-        if (more) {
+    uint32_t t0 = t_begin;
+    for (; t0 + kPrefixTile <= t_end; t0 += kPrefixTile) {
+        __syncthreads();                      // the tile before it is done with
+        put();
+        __syncthreads();
+        if (t0 + kPrefixTile < t_end) {
             fetch(t0 + kPrefixTile);
             look_up(t0 + 2 * kPrefixTile);
         }
-        const bool tail = t0 + kPrefixTile > t_end;
-        const uint8_t *kt = smem[buf][0], *vt = smem[buf][1];
-#pragma unroll
-        for (int step = 0; step < TT; step += STEP) {
-            const uint32_t tb = 16u * (wt * TT + step);
-            // S^T = K . Q^T
-            f32x4_t s[2][STEP];
-#pragma unroll
-            for (int u = 0; u < STEP; ++u) {
-                const uint32_t t = tb + 16u * u + r16;
-                s[0][u] = s[1][u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const u32x4 kf = *reinterpret_cast<const u32x4 *>(kt + t * RB + 16u * ((4u * ks + g4) ^ swz(t)));
-                    s[0][u] = mfma_qk<BF16>(kf, qf[0][ks], s[0][u]);
-                    s[1][u] = mfma_qk<BF16>(kf, qf[1][ks], s[1][u]);
-                }
-            }
-            // softmax of query row r16 of each column block over the lane's
-            // tokens tb + 16 * u + 4 * g4 + i.  The maximum that weights are
-            // taken against moves only when a score exceeds it by 2^8: the
-            // sums have the room, and the accumulators are rescaled seldom.
-            uint32_t ph[2][STEP][2], pl[2][STEP][2];
-            if (tail)
-#pragma unroll
-                for (int u = 0; u < STEP; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (t0 + tb + 16u * u + 4u * g4 + i >= t_end)
-                            s[0][u][i] = s[1][u][i] = -INFINITY;
-#pragma unroll
-            for (int rt = 0; rt < 2; ++rt) {
-                float mx = -INFINITY;
-#pragma unroll
-                for (int u = 0; u < STEP; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        mx = fmaxf(mx, s[rt][u][i]);
-                mx *= qk_scale;
-                if (__ballot(mx > m[rt] + 8.f)) {
-                    const float m_new = fmaxf(m[rt], max_of_rows(mx));
-                    const float c = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[rt] - m_new);
-                    lsum[rt] *= c;
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
-                        acc[rt][mt] = acc[rt][mt] * c;
-                    m[rt] = m_new;
-                }
-                const float m_sub = m[rt] == -INFINITY ? 0.f : m[rt];
-#pragma unroll
-                for (int u = 0; u < STEP; ++u) {
-                    float p[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        p[i] = __builtin_amdgcn_exp2f(s[rt][u][i] * qk_scale - m_sub);
-                    if (tail)       // (a scale of 0 would make NaN of the mask's -inf)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            p[i] = t0 + tb + 16u * u + 4u * g4 + i < t_end ? p[i] : 0.f;
-                    lsum[rt] += (p[0] + p[1]) + (p[2] + p[3]);
-                    split_weights<BF16>(p[0], p[1], &ph[rt][u][0], &pl[rt][u][0]);
-                    split_weights<BF16>(p[2], p[3], &ph[rt][u][1], &pl[rt][u][1]);
-                }
-            }
-            // O^T += V^T . P^T, the weights as their 16-bit rounding and the
-            // 16-bit rounding of the rest
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                uint64_t vf[STEP];
-#pragma unroll
-                for (int u = 0; u < STEP; ++u) {
-                    const uint32_t t = tb + 16u * u + 4u * g4 + r16 / 4u;
-                    const uint32_t c = 2u * mt + r16 % 4u / 2u;
-                    vf[u] = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (LLMIG_LDS i16x4_t *)(vt + t * RB + 16u * (c ^ swz(t)) + 8u * (r16 % 2u))));
-                }
-                typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
-                const u32x4 v = __builtin_bit_cast(u32x4, u64x2{vf[0], vf[STEP - 1]});
-#pragma unroll
-                for (int rt = 0; rt < 2; ++rt) {
-                    const uint32_t(&h)[STEP][2] = ph[rt], (&l)[STEP][2] = pl[rt];
-                    if constexpr (STEP == 2) {
-                        acc[rt][mt] = mfma_qk<BF16>(v, u32x4{h[0][0], h[0][1], h[1][0], h[1][1]}, acc[rt][mt]);
-                        acc[rt][mt] = mfma_qk<BF16>(v, u32x4{l[0][0], l[0][1], l[1][0], l[1][1]}, acc[rt][mt]);
-                    } else {        // 16 tokens: both parts in one product, against the same V rows twice
-                        acc[rt][mt] = mfma_qk<BF16>(v, u32x4{h[0][0], h[0][1], l[0][0], l[0][1]}, acc[rt][mt]);
-                    }
-                }
-            }
-        }
-        if (more)
-            put(buf ^ 1u);
+        work(t0, std::false_type());
+    }
+    if (t0 < t_end) {
+        __syncthreads();
+        put();
+        __syncthreads();
+        work(t0, std::true_type());
     }
 
     // The wavefronts that split the tokens meet in LDS, 16 rows of each at a
     // time, and the records leave in whole rows.
+    lsum = sum_of_halves(lsum);
+    if (half == 0) {
+        sh_m[wave][l32] = m;
+        sh_l[wave][l32] = lsum;
+    }
+    float *so = reinterpret_cast<float *>(&smem[0][0]);           // [wave][16 rows][kMergeRow]
 #pragma unroll
-    for (int rt = 0; rt < 2; ++rt)
-        lsum[rt] = sum_of_rows(lsum[rt]);
-    float *so = reinterpret_cast<float *>(&smem[0][0][0]);        // [wave][16 rows][kMergeRow]
-#pragma unroll
-    for (int rt = 0; rt < 2; ++rt) {
+    for (uint32_t rt = 0; rt < 2; ++rt) {
         __syncthreads();
+        if (l32 / 16u == rt) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-            *reinterpret_cast<f32x4_t *>(so + (wave * 16u + r16) * kMergeRow + 16 * mt + 4 * g4) = acc[rt][mt];
-        if (g4 == 0) {
-            sh_m[wave][16 * rt + r16] = m[rt];
-            sh_l[wave][16 * rt + r16] = lsum[rt];
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<f32x4_t *>(so + (wave * 16u + r16) * kMergeRow + 32 * mt + 8 * i + 4 * half) =
+                        f32x4_t{acc[mt][4 * i], acc[mt][4 * i + 1], acc[mt][4 * i + 2], acc[mt][4 * i + 3]};
         }
         __syncthreads();
         for (uint32_t x = threadIdx.x; x < WM * 16u * (D / 4); x += kThreads) {
@@ -413,19 +451,25 @@ inline const void *prefix_join_kernel(int head_dim, uint32_t most, uint32_t *row
     return most <= 8 ? reinterpret_cast<const void *>(&prefix_join<128, 1>) : reinterpret_cast<const void *>(&prefix_join<128, 8>);
 }
 
-template <int BF16, int D>
+template <int BF16, int D, int ALIGNED>
 const void *prefix_kernel(uint32_t wm)
 {
-    return wm == 1   ? reinterpret_cast<const void *>(&prefix_rows<BF16, D, 1>)
-           : wm == 2 ? reinterpret_cast<const void *>(&prefix_rows<BF16, D, 2>)
-                     : reinterpret_cast<const void *>(&prefix_rows<BF16, D, 4>);
+    return wm == 1   ? reinterpret_cast<const void *>(&prefix_rows<BF16, D, 1, ALIGNED>)
+           : wm == 2 ? reinterpret_cast<const void *>(&prefix_rows<BF16, D, 2, ALIGNED>)
+                     : reinterpret_cast<const void *>(&prefix_rows<BF16, D, 4, ALIGNED>);
 }
 
-inline const void *prefix_kernel_for(int bf16, int head_dim, uint32_t wm)
+template <int BF16, int D>
+const void *prefix_kernel(uint32_t wm, bool aligned)
+{
+    return aligned ? prefix_kernel<BF16, D, 1>(wm) : prefix_kernel<BF16, D, 0>(wm);
+}
+
+inline const void *prefix_kernel_for(int bf16, int head_dim, uint32_t wm, bool aligned)
 {
     if (head_dim == 64)
-        return bf16 ? prefix_kernel<1, 64>(wm) : prefix_kernel<0, 64>(wm);
-    return bf16 ? prefix_kernel<1, 128>(wm) : prefix_kernel<0, 128>(wm);
+        return bf16 ? prefix_kernel<1, 64>(wm, aligned) : prefix_kernel<0, 64>(wm, aligned);
+    return bf16 ? prefix_kernel<1, 128>(wm, aligned) : prefix_kernel<0, 128>(wm, aligned);
 }
 
 // How the prefix of a call is cut: wavefronts of a workgroup that split the
