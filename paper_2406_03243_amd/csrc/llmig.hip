@@ -1492,12 +1492,16 @@ static int prefix_plan(const llmig_pool *pool, const int32_t *ctx_lens, int32_t 
     }
     if (p->members < 2)
         p->members = 0;
+    if (p->members) {
+        p->cut = prefix_cut(p->members * static_cast<uint32_t>(q_heads / H), tokens, L * H, D);
+        if (!prefix_pays(p->cut, p->members, q_heads / H, tokens, L, H, D))
+            p->members = 0;
+    }
     for (int32_t b = 0; b < batch; ++b)
         p->own[b] = p->members && ctx_lens[b] >= tokens ? static_cast<int32_t>(ctx_lens[b] - tokens) : ctx_lens[b];
     p->part = attn_part_tokens(p->own, batch, L, H, D);
     if (!p->members)
         return attn_record_bytes(p->own, batch, p->part, L, q_heads, D, &p->own_bytes);
-    p->cut = prefix_cut(p->members * static_cast<uint32_t>(q_heads / H), tokens, L * H);
     int64_t v = 0;
     if (__builtin_mul_overflow(attn_items(p->own, batch, p->part), L * q_heads, &v) ||
         __builtin_mul_overflow(v, (D + kAttnHeader) * 4, &p->own_bytes) ||
@@ -1940,7 +1944,7 @@ int llmig_decode_attention_prefix(const llmig_pool *pool, int32_t dtype, const v
         j.member[s] = place[r.seq[s]];
     }
     uint32_t per = 0;
-    const void *jfn = prefix_join_kernel(pool->head_dim, most + p.cut.parts, &per);
+    const void *jfn = prefix_join_kernel(pool->head_dim, rows, most + p.cut.parts, &per);
     for (uint64_t at = 0; at < rows; at += static_cast<uint64_t>(kMaxGridWorkgroups) * per) {
         j.row_base = static_cast<uint32_t>(at);
         void *jargs[] = {&j};

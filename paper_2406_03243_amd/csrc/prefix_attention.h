@@ -18,7 +18,13 @@
 
 namespace {
 
-constexpr uint32_t kPrefixTile = 128;     // tokens of K and V in LDS at a time
+// Tokens of K and V in LDS at a time, for wm wavefronts along the rows: few rows
+// wait for memory and want much of it in flight, many for the matrix cores and
+// want the registers.
+constexpr uint32_t prefix_tile(uint32_t wm)
+{
+    return wm >= 2 ? 64 : 128;
+}
 
 struct PrefixArgs {
     const uint64_t *tab;         // pool table: K bases then V bases
@@ -28,7 +34,7 @@ struct PrefixArgs {
     float scale;
     uint32_t num_layers, batch, q_heads, kv_heads, num_blocks, block_size;
     uint32_t tokens;             // of the prefix
-    uint32_t part_tokens, parts; // a partition's tokens (a multiple of kPrefixTile), partitions
+    uint32_t part_tokens, parts; // a partition's tokens (a multiple of its tile), partitions
     uint32_t members;            // sequences behind the prefix
     uint32_t chunks;             // workgroups that share a partition's rows
     Divisor by_block;
@@ -106,13 +112,15 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
     constexpr uint32_t LPR = D / 8;                // 16-byte chunks of a row
     constexpr uint32_t RB = D * 2;                 // bytes of a row
     constexpr uint32_t RPB = 128 / D;              // rows per 256 bytes
-    constexpr int CPT = kPrefixTile * LPR / kThreads;    // chunks of K, and of V, a thread brings per tile
+    constexpr uint32_t T = prefix_tile(WM), BUFS = T == 64 ? 2 : 1;
+    constexpr int STEPS = T * WM / 128;            // of 32 tokens a wavefront takes of a tile
+    constexpr int CPT = T * LPR / kThreads;    // chunks of K, and of V, a thread brings per tile
     constexpr uint32_t RPI = kThreads / LPR;       // rows that the threads bring at a time
     constexpr float kLog2e = 1.4426950408889634f;
-    constexpr uint32_t kTileBytes = kPrefixTile * RB;
+    constexpr uint32_t kTileBytes = T * RB;
     constexpr uint32_t kMergeRow = D + 4;
-    __shared__ __align__(16) uint8_t smem[2][kTileBytes];         // K, V
-    static_assert(4 * 16 * kMergeRow * 4 <= 2 * kTileBytes, "the merge of 16 rows fits");
+    __shared__ __align__(16) uint8_t smem[BUFS][2][kTileBytes];   // K, V
+    static_assert(4 * 16 * kMergeRow * 4 <= 2 * BUFS * kTileBytes, "the merge of 16 rows fits");
     __shared__ float sh_m[4][32], sh_l[4][32];
 
     // The workgroups that read the same tokens (a partition's row chunks, then
@@ -188,11 +196,11 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
     auto v_swizzle = [](uint32_t t) { return t / RPB % (4u / RPB) * 4u ^ t / 4u % 4u; };
     static_assert(RPI % 16 == 0, "a thread's rows swizzle alike");
     const uint32_t put_k = th * RB + 16u * (tc ^ k_swizzle(th)), put_v = th * RB + 16u * (tc ^ v_swizzle(th));
-    auto put = [&]() {
+    auto put = [&](uint32_t buf) {
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
-            *reinterpret_cast<u32x4 *>(&smem[0][put_k + i * RPI * RB]) = kr[i];
-            *reinterpret_cast<u32x4 *>(&smem[1][put_v + i * RPI * RB]) = vr[i];
+            *reinterpret_cast<u32x4 *>(&smem[buf][0][put_k + i * RPI * RB]) = kr[i];
+            *reinterpret_cast<u32x4 *>(&smem[buf][1][put_v + i * RPI * RB]) = vr[i];
         }
     };
 
@@ -215,27 +223,32 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
             acc[mt][i] = 0.f;
 
     // A tile in LDS; TAIL: the partition ends in it.
-    auto work = [&](uint32_t t0, auto tail_c) {
+    auto work = [&](uint32_t buf, uint32_t t0, auto tail_c) {
         constexpr bool TAIL = decltype(tail_c)::value;
-        const uint8_t *kt = smem[0] + wt * (32u * WM) * RB, *vt = smem[1] + wt * (32u * WM) * RB;
-        // S^T = K . Q^T of 32 tokens
-        auto scores = [&](int step) {
-            f32x16_t s;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                s[i] = 0.f;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const u32x4 kf = *reinterpret_cast<const u32x4 *>(kt + 32 * step * RB + k_at + (k_x ^ (32u * ks)));
-                s = mfma_32<BF16>(kf, qf[ks], s);
-            }
-            return s;
+        const uint8_t *kt = smem[buf][0] + wt * (32u * STEPS) * RB, *vt = smem[buf][1] + wt * (32u * STEPS) * RB;
+        auto k_rows = [&](int step, int ks) {
+            return *reinterpret_cast<const u32x4 *>(kt + 32 * step * RB + k_at + (k_x ^ (32u * ks)));
         };
-        f32x16_t s = scores(0);
+        auto v_rows = [&](int step, int n, int mt) {
+            typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+            u64x2 v;
 #pragma unroll
-        for (int step = 0; step < WM; ++step) {
+            for (uint32_t j = 0; j < 2; ++j)
+                v[j] = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (LLMIG_LDS i16x4_t *)(vt + (32 * step + 16 * n + 8 * j) * RB + v_at + (v_x ^ (64u * mt) ^ (32u * j)))));
+            return __builtin_bit_cast(u32x4, v);
+        };
+        f32x16_t s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            s[i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+            s = mfma_32<BF16>(k_rows(0, ks), qf[ks], s);
+#pragma unroll
+        for (int step = 0; step < STEPS; ++step) {
             // element i of s is token first + 8 * (i / 4) + i % 4, of query row l32
-            const uint32_t first = t0 + 32u * (wt * WM + step) + 4u * half;
+            const uint32_t first = t0 + 32u * (wt * STEPS + step) + 4u * half;
             if constexpr (TAIL) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
@@ -258,72 +271,92 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
                     acc[mt] = acc[mt] * c;
                 m = m_new;
             }
-            f32x16_t s_next;
-            if (step + 1 < WM)
-                s_next = scores(step + 1);
             const float m_sub = m == -INFINITY ? 0.f : m;
-            float p[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                p[i] = __builtin_amdgcn_exp2f(s[i] * qk_scale - m_sub);
-            if constexpr (TAIL) {       // (a scale of 0 would make NaN of the mask's -inf)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    p[i] = first + 8u * (i / 4) + i % 4 < t_end ? p[i] : 0.f;
-            }
+            // From here on to the end of the step products and weights alternate:
+            // the next 32 tokens' scores beside the first 16 tokens' weights, those
+            // tokens' part of O^T += V^T . P^T beside the other 16 tokens' weights.
             uint32_t hi[8], lo[8];
+            auto weights = [&](int n) {
+                float p[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                lsum += p[2 * i] + p[2 * i + 1];
-                split_weights<BF16>(p[2 * i], p[2 * i + 1], &hi[i], &lo[i]);
-            }
-            // O^T += V^T . P^T, 16 tokens at a time, the weights as their 16-bit
-            // rounding and the 16-bit rounding of the rest
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                u32x4 vf[MT];
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    uint64_t v[2];
-#pragma unroll
-                    for (uint32_t j = 0; j < 2; ++j)
-                        v[j] = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (LLMIG_LDS i16x4_t *)(vt + (32 * step + 16 * n + 8 * j) * RB + v_at +
-                                                  (v_x ^ (64u * mt) ^ (32u * j)))));
-                    typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
-                    vf[mt] = __builtin_bit_cast(u32x4, u64x2{v[0], v[1]});
+                for (int i = 0; i < 8; ++i) {
+                    const int k = 8 * n + i;
+                    p[i] = __builtin_amdgcn_exp2f(s[k] * qk_scale - m_sub);
+                    if constexpr (TAIL)         // (a scale of 0 would make NaN of the mask's -inf)
+                        p[i] = first + 8u * (k / 4) + k % 4 < t_end ? p[i] : 0.f;
                 }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    lsum += p[2 * i] + p[2 * i + 1];
+                    split_weights<BF16>(p[2 * i], p[2 * i + 1], &hi[4 * n + i], &lo[4 * n + i]);
+                }
+            };
+            // the weights as their 16-bit rounding and the 16-bit rounding of the rest
+            auto values = [&](int n, const u32x4 *vf) {
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
                     acc[mt] = mfma_32<BF16>(vf[mt], u32x4{hi[4 * n], hi[4 * n + 1], hi[4 * n + 2], hi[4 * n + 3]}, acc[mt]);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
                     acc[mt] = mfma_32<BF16>(vf[mt], u32x4{lo[4 * n], lo[4 * n + 1], lo[4 * n + 2], lo[4 * n + 3]}, acc[mt]);
+            };
+            u32x4 v0[MT], v1[MT];
+            f32x16_t s_next;
+            const bool next = step + 1 < STEPS;
+            if (next) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    s_next[i] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+                    s_next = mfma_32<BF16>(k_rows(step + 1, ks), qf[ks], s_next);
             }
-            if (step + 1 < WM)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+                v0[mt] = v_rows(step, 0, mt);
+            weights(0);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+                v1[mt] = v_rows(step, 1, mt);
+            values(0, v0);
+            weights(1);
+            values(1, v1);
+            if (next)
                 s = s_next;
         }
     };
 
     look_up(t_begin);
     fetch(t_begin);
-    look_up(t_begin + kPrefixTile);
-    uint32_t t0 = t_begin;
-    for (; t0 + kPrefixTile <= t_end; t0 += kPrefixTile) {
+    look_up(t_begin + T);
+    uint32_t t0 = t_begin, buf = 0;
+    if constexpr (BUFS == 2)
+        put(0);
+    for (; t0 + T <= t_end; t0 += T) {
         __syncthreads();                      // the tile before it is done with
-        put();
-        __syncthreads();
-        if (t0 + kPrefixTile < t_end) {
-            fetch(t0 + kPrefixTile);
-            look_up(t0 + 2 * kPrefixTile);
+        if constexpr (BUFS == 1) {
+            put(0);
+            __syncthreads();
         }
-        work(t0, std::false_type());
+        const bool more = t0 + T < t_end;
+        if (more) {
+            fetch(t0 + T);
+            look_up(t0 + 2 * T);
+        }
+        work(buf, t0, std::false_type());
+        if constexpr (BUFS == 2) {
+            buf ^= 1u;
+            if (more)
+                put(buf);
+        }
     }
     if (t0 < t_end) {
         __syncthreads();
-        put();
-        __syncthreads();
-        work(t0, std::true_type());
+        if constexpr (BUFS == 1) {
+            put(0);
+            __syncthreads();
+        }
+        work(buf, t0, std::true_type());
     }
 
     // The wavefronts that split the tokens meet in LDS, 16 rows of each at a
@@ -333,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
         sh_m[wave][l32] = m;
         sh_l[wave][l32] = lsum;
     }
-    float *so = reinterpret_cast<float *>(&smem[0][0]);           // [wave][16 rows][kMergeRow]
+    float *so = reinterpret_cast<float *>(&smem[0][0][0]);         // [wave][16 rows][kMergeRow]
 #pragma unroll
     for (uint32_t rt = 0; rt < 2; ++rt) {
         __syncthreads();
@@ -442,13 +475,18 @@ __global__ void __launch_bounds__(kThreads) prefix_join(const PrefixJoinArgs a)
             l > 0.f ? acc / l : f32x4_t{0.f, 0.f, 0.f, 0.f};
 }
 
-// The join for at most `most` records a row; its rows per workgroup.
-inline const void *prefix_join_kernel(int head_dim, uint32_t most, uint32_t *rows)
+// The join of `rows` rows of at most `most` records; its rows per workgroup.
+// Side by side where the rows alone leave the chip empty.
+inline const void *prefix_join_kernel(int head_dim, uint64_t rows, uint32_t most, uint32_t *per)
 {
-    *rows = kThreads / (head_dim / 4) / (most <= 8 ? 1u : 8u);
-    if (head_dim == 64)
-        return most <= 8 ? reinterpret_cast<const void *>(&prefix_join<64, 1>) : reinterpret_cast<const void *>(&prefix_join<64, 8>);
-    return most <= 8 ? reinterpret_cast<const void *>(&prefix_join<128, 1>) : reinterpret_cast<const void *>(&prefix_join<128, 8>);
+    *per = kThreads / (head_dim / 4);
+    if (most > 8 && rows / *per < 512) {
+        *per /= 8;
+        return head_dim == 64 ? reinterpret_cast<const void *>(&prefix_join<64, 8>)
+                              : reinterpret_cast<const void *>(&prefix_join<128, 8>);
+    }
+    return head_dim == 64 ? reinterpret_cast<const void *>(&prefix_join<64, 1>)
+                          : reinterpret_cast<const void *>(&prefix_join<128, 1>);
 }
 
 template <int BF16, int D, int ALIGNED>
@@ -473,22 +511,68 @@ inline const void *prefix_kernel_for(int bf16, int head_dim, uint32_t wm, bool a
 }
 
 // How the prefix of a call is cut: wavefronts of a workgroup that split the
-// rows, workgroups that share a partition, partitions.
+// rows, workgroups that share a partition, partitions; and about how long that
+// takes.
 struct PrefixCut {
     uint32_t wm, chunks, part_tokens, parts;
+    int64_t ns;
 };
 
-inline PrefixCut prefix_cut(uint32_t rows, int64_t tokens, int64_t layer_heads)
+// Partitions fill the chip, two workgroups a CU; each costs a record per row,
+// written and read again.  What a cut takes was measured for 18 shapes (1 to 32
+// layers, 4 to 32 heads, 8 to 512 rows, prefixes of 512 to 16384 tokens, 1 to 64
+// partitions) and is, in rounds of 512 workgroups,
+//     3 us + tiles of a partition x 1.4 us (x 1.6 with two a CU) + 0.35 ns a record,
+// for head_dim 128: the partitions that this puts first were within 1.4% of the
+// best ones on average, 7.4% at most (8 heads, 512 rows, 8192 tokens: 1 partition
+// 231 us, 4 76, 8 53.6, 12 58, 32 74).
+constexpr int64_t kPrefixStartNs = 3000, kPrefixTileNs = 1400;
+constexpr uint32_t kPrefixMostParts = 128;
+
+inline int64_t prefix_cut_ns(int64_t workgroups, int64_t tiles, int64_t records, int64_t head_dim)
+{
+    const int64_t rounds = (workgroups + 511) / 512, last = workgroups - (rounds - 1) * 512;
+    const int64_t work = tiles * kPrefixTileNs * (128 + head_dim) / 256;
+    return rounds * kPrefixStartNs + work * ((rounds - 1) * 16 + (last <= 256 ? 10 : 16)) / 10 +
+           records * head_dim * 35 / 12800;
+}
+
+inline PrefixCut prefix_cut(uint32_t rows, int64_t tokens, int64_t layer_heads, int64_t head_dim)
 {
     PrefixCut c;
     c.wm = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
     c.chunks = (rows + 32 * c.wm - 1) / (32 * c.wm);
-    const int64_t tiles = (tokens + kPrefixTile - 1) / kPrefixTile;
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(tiles, 512 / std::max<int64_t>(1, layer_heads * c.chunks)));
-    const int64_t per = (tiles + want - 1) / want;
-    c.part_tokens = static_cast<uint32_t>(per * kPrefixTile);
-    c.parts = static_cast<uint32_t>((tiles + per - 1) / per);
+    c.ns = -1;
+    const uint32_t tile = prefix_tile(c.wm);
+    const int64_t tiles = (tokens + tile - 1) / tile, most = std::min<int64_t>(tiles, kPrefixMostParts);
+    for (int64_t want = 1; want <= most; ++want) {
+        const int64_t per = (tiles + want - 1) / want, parts = (tiles + per - 1) / per;
+        const int64_t ns = prefix_cut_ns(parts * layer_heads * c.chunks, per, parts * rows * layer_heads, head_dim);
+        if (parts == want && (c.ns < 0 || ns < c.ns)) {
+            c.ns = ns;
+            c.parts = static_cast<uint32_t>(parts);
+            c.part_tokens = static_cast<uint32_t>(per * tile);
+        }
+    }
     return c;
+}
+
+// Whether reading the prefix once pays.  It costs one launch more than plain
+// attention, and every row leaves a record of its own tokens, too.  Plain attention
+// reads the prefix for each of `members` sequences, after the first mostly out of
+// the caches: 10 to 14 TB/s where an XCD's share of the layers fits into its L2,
+// 7 to 10 else.  Prefix / plain, us: one layer of 8 heads of 128 and 4 query heads
+// each, 7 sequences behind 2000 tokens 18.0 / 15.7, 8 behind 8192 23 / 32, 64 behind
+// 512 23.5 / 17.8; 8 query heads each, 32 behind 2000 33 / 30, 64 behind 2000 36 / 74;
+// 8 layers, 32 behind 128 34 / 22, 8 behind 512 20 / 17, 32 behind 512 40 / 48, 8
+// behind 2000 28 / 70.
+inline bool prefix_pays(const PrefixCut &c, int64_t members, int64_t group, int64_t tokens, int64_t layers, int64_t heads,
+                        int64_t head_dim)
+{
+    const double layer_bytes = static_cast<double>(tokens) * heads * head_dim * 4;
+    const bool cached = layer_bytes * std::max<int64_t>(1, layers / 8) <= 4 << 20;
+    const double plain_ns = layer_bytes * layers * members / (cached ? 12500. : 8500.);
+    return c.ns + 6500 + members * group * layers * heads * head_dim * 35 / 12800 < plain_ns;
 }
 
 } // namespace

@@ -1,0 +1,144 @@
+"""Runs calls of the operators for long contexts over a stand-in HIP runtime
+(fake_hip.c) and prints, as JSON, what each returns and which kernels it
+launches.  A process of its own, without torch:
+
+    python operator_calls.py FAKE_HIP.so LIBLLMIG.so < calls.json
+
+A call is {"op": name, ...}: the arguments that differ from those of a small
+valid call.  Device addresses are numbers that nothing reads."""
+import ctypes
+import json
+import re
+import sys
+
+import numpy as np
+
+U32, I32, I64, U64, P = ctypes.c_uint32, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_void_p
+
+
+class Desc(ctypes.Structure):
+    _fields_ = [(n, I32) for n in ("num_layers", "num_blocks", "block_size", "num_kv_heads", "head_dim", "elem_bytes")] \
+        + [("k_ptrs", ctypes.POINTER(U64)), ("v_ptrs", ctypes.POINTER(U64)), ("k_layout", I32), ("v_layout", I32)]
+
+
+class Append(ctypes.Structure):
+    _fields_ = [("dtype", I32), ("batch", I32), ("q_heads", I32), ("table_stride", I32), ("q", P), ("k", P), ("v", P),
+                ("q_out", P), ("q_layer", I64), ("q_token", I64), ("k_layer", I64), ("k_token", I64), ("v_layer", I64),
+                ("v_token", I64), ("tables", P), ("from_toks", P), ("n_toks", P), ("first_pos", P), ("cos_sin", P),
+                ("positions", I32), ("rotary_dim", I32), ("interleaved", I32)]
+
+
+launches = []
+
+
+@ctypes.CFUNCTYPE(None, ctypes.c_char_p, ctypes.POINTER(U32), U64, ctypes.c_void_p)
+def on_launch(name, gb, lds, args):
+    m = re.search(r"\d+([a-z]+_[a-z_]+?)(?:I|E|N)", name.decode().split("GLOBAL__N_1")[-1])
+    launches.append({"kernel": m.group(1), "grid": gb[0], "block": gb[3],
+                     "template": [int(x) for x in re.findall(r"Li(\d+)E", name.decode())]})
+
+
+fake = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
+fake.fake_hip_on_launch(on_launch)
+lib = ctypes.CDLL(sys.argv[2])
+pools = {}
+
+
+def pool(layers=1, blocks=64, bs=16, heads=2, dim=64, elem=2, layouts=(0, 0), at=1):
+    key = (layers, blocks, bs, heads, dim, elem, tuple(layouts), at)
+    if key not in pools:
+        size = (blocks * bs * heads * dim * elem + 255) // 256 * 256
+        ptr = [(at << 43) + i * size for i in range(2 * layers)]
+        desc = Desc(layers, blocks, bs, heads, dim, elem, (U64 * layers)(*ptr[:layers]), (U64 * layers)(*ptr[layers:]),
+                    *layouts)
+        h = P()
+        assert lib.llmig_pool_create(ctypes.byref(desc), ctypes.byref(h)) == 0
+        pools[key] = h
+    return pools[key]
+
+
+def lens(x):
+    return None if x is None else np.asarray(x, np.int32)
+
+
+def at(a):
+    return None if a is None else P(a.ctypes.data)
+
+
+def dev(n):
+    return P(n) if n else None
+
+
+A = [0] + [k << 44 for k in range(1, 8)]      # device addresses
+
+
+def append(pool_args=None, no_pool=False, from_toks=(5, 0), n_toks=(1, 20), first_pos=None, **kw):
+    f, n, p = lens(from_toks), lens(n_toks), lens(first_pos)
+    pool_args = pool_args or {}
+    row = pool_args.get("heads", 2) * pool_args.get("dim", 64)
+    d = dict(dtype=1, batch=0 if n is None else len(n), q_heads=4, table_stride=4, q=A[1], k=A[2], v=A[3], q_out=A[4],
+             q_layer=2 * row * 21, q_token=2 * row, k_layer=row * 21, k_token=row, v_layer=row * 21, v_token=row,
+             tables=A[5], cos_sin=A[6], positions=100, rotary_dim=64, interleaved=0)
+    d.update(kw)
+    desc = Append(from_toks=f.ctypes.data if f is not None else None, n_toks=n.ctypes.data if n is not None else None,
+                  first_pos=p.ctypes.data if p is not None else None, **d)
+    return lib.llmig_append_rotary(None if no_pool else pool(**pool_args), ctypes.byref(desc), None), None
+
+
+def bounds(pool_args=None, bounds_args=None, no_pool=False, no_bounds=False, dtype=1, batch=2, tables=A[1], table_stride=4,
+           from_toks=(5, 0), ctx_lens=(6, 40)):
+    f, c = lens(from_toks), lens(ctx_lens)
+    b = dict(bs=1, at=2)
+    b.update(bounds_args or {})
+    return lib.llmig_key_bounds(None if no_pool else pool(**(pool_args or {})), None if no_bounds else pool(**b), dtype,
+                                batch, dev(tables), table_stride, at(f), at(c), None), None
+
+
+def select(bounds_args=None, no_bounds=False, dtype=1, block_size=16, q=A[1], batch=2, q_heads=4, tables=A[2],
+           table_stride=8, ctx_lens=(100, 40), keep_first=1, keep_last=1, count=4, workspace=A[3], less=0, blocks=A[4]):
+    c = lens(ctx_lens)
+    b = dict(bs=1, at=2)
+    b.update(bounds_args or {})
+    p = None if no_bounds else pool(**b)
+    n = I64(-1)
+    rc = lib.llmig_select_blocks_workspace(p, block_size, at(c), batch, ctypes.byref(n))
+    return lib.llmig_select_blocks(p, dtype, block_size, dev(q), batch, q_heads, dev(tables), table_stride, at(c), keep_first,
+                                   keep_last, count, dev(workspace), I64(max(0, n.value) - less), dev(blocks), None), n.value
+
+
+def attend(pool_args=None, no_pool=False, dtype=1, q=A[1], batch=2, q_heads=4, tables=A[2], table_stride=8,
+           ctx_lens=(100, 40), blocks=A[4], count=4, workspace=A[3], less=0, out=A[5]):
+    c = lens(ctx_lens)
+    p = None if no_pool else pool(**(pool_args or {}))
+    n = I64(-1)
+    lib.llmig_decode_attention_blocks_workspace(p, at(c), batch, q_heads, count, ctypes.byref(n))
+    return lib.llmig_decode_attention_blocks(p, dtype, dev(q), batch, q_heads, dev(tables), table_stride, at(c), dev(blocks),
+                                             count, ctypes.c_float(0.1), dev(workspace), I64(max(0, n.value) - less),
+                                             dev(out), None), n.value
+
+
+def prefix(pool_args=None, no_pool=False, dtype=1, q=A[1], batch=None, q_heads=4, tables=A[2], table_stride=8,
+           ctx_lens=(100, 70), prefix_blocks=4, workspace=A[3], less=0, out=A[5]):
+    c = lens(ctx_lens)
+    batch = (0 if c is None else len(c)) if batch is None else batch
+    p = None if no_pool else pool(**(pool_args or {}))
+    n = I64(-1)
+    lib.llmig_decode_attention_prefix_workspace(p, at(c), batch, q_heads, prefix_blocks, ctypes.byref(n))
+    return lib.llmig_decode_attention_prefix(p, dtype, dev(q), batch, q_heads, dev(tables), table_stride, at(c),
+                                             prefix_blocks, ctypes.c_float(0.1), dev(workspace),
+                                             I64(max(0, n.value) - less), dev(out), None), n.value
+
+
+OPS = {f.__name__: f for f in (append, bounds, select, attend, prefix)}
+
+
+def main():
+    results = []
+    for c in json.load(sys.stdin):
+        launches.clear()
+        rc, workspace = OPS[c.pop("op")](**c)
+        results.append({"rc": rc, "workspace": workspace, "launches": list(launches)})
+    json.dump(results, sys.stdout)
+
+
+main()

@@ -1,5 +1,10 @@
 """Decode attention of a batch behind a shared prefix against attention in 64
-bits (reference and bound: tests/operator_cases.py)."""
+bits (reference and bound: tests/operator_cases.py).
+
+Short prefixes and small batches run as plain attention.  The lengths here stay
+below the 768 tokens from which plain attention would want a workspace (or the
+case says so), so the workspace's size tells which way a call goes; SHARED lists
+cases that read the prefix once, of every variant of that kernel."""
 import math
 
 import pytest
@@ -34,12 +39,14 @@ def setup(L, H, G, D, bs, dtype, ctx, prefix, seed=1):
     return kv, q, tables
 
 
-def run(kv, q, tables, ctx, prefix, dtype, scale=None, stream=None):
+def run(kv, q, tables, ctx, prefix, dtype, scale=None, once=None):
     L, B, HQ, D = q.shape
     scale = 1 / math.sqrt(D) if scale is None else scale
     dev = kv.cuda()
     pool = Pool(list(dev[0].unbind(0)), list(dev[1].unbind(0)))
     nbytes = decode_prefix_workspace_bytes(pool, ctx, HQ, prefix)
+    if once is not None:
+        assert (nbytes > 0) == once
     ws = torch.full((nbytes + 32,), 0xFF, dtype=torch.uint8, device="cuda")     # NaN patterns
     out = torch.full((L, B + 1, HQ, D), 7.0, device="cuda")
     mine = torch.full(q.shape, 7.0, device="cuda")
@@ -80,69 +87,106 @@ def test_matches_attention(case):
     run(*setup(L, H, G, D, bs, dtype, ctx, prefix), ctx, prefix, dtype)
 
 
+# Up to 32, up to 64 and more rows a KV head; one workgroup a partition and two;
+# blocks of 16 tokens or a multiple, and others; prefixes that end inside a tile.
+SHARED = [
+    (1, 16, 1, 128, 16, "bf16", [688 + i for i in range(30)], 43),
+    (1, 16, 1, 128, 12, "fp16", [684 + 2 * i for i in range(30)], 57),
+    (1, 16, 4, 128, 32, "bf16", [736 + (i % 3) for i in range(8)] + [1300] * 24, 23),
+    (1, 64, 2, 64, 48, "fp16", [672 + i for i in range(16)], 14),
+    (1, 32, 1, 64, 1, "bf16", [600 + i for i in range(32)], 600),
+    (1, 8, 1, 128, 16, "fp16", [704 + (i % 40) for i in range(60)], 44),
+    (1, 8, 1, 128, 24, "bf16", [720 + (i % 40) for i in range(60)], 30),
+    (1, 8, 2, 128, 16, "bf16", [656 + (i % 7) for i in range(100)], 41),
+    (1, 8, 2, 128, 20, "fp16", [660 + (i % 7) for i in range(100)], 33),
+    (2, 16, 4, 64, 16, "bf16", [720 + (i % 9) for i in range(60)], 45),
+    (2, 16, 4, 64, 8, "fp16", [720 + (i % 9) for i in range(60)], 90),
+    (3, 4, 4, 128, 16, "bf16", [700, 0, 699, 41, 0, 688, 687] + [688] * 60, 43),     # some share nothing, some end there
+]
+
+
+@pytest.mark.parametrize("case", SHARED, ids=lambda c: f"L{c[0]}_H{c[1]}_G{c[2]}_D{c[3]}_bs{c[4]}_{c[5]}_B{len(c[6])}_p{c[7]}")
+def test_reads_the_prefix_once(case):
+    print("[case]", case, flush=True)
+    L, H, G, D, bs, dtype, ctx, prefix = case
+    run(*setup(L, H, G, D, bs, dtype, ctx, prefix), ctx, prefix, dtype, once=True)
+
+
+def test_long_prefix_in_several_partitions():
+    ctx = [5000 + 3 * i for i in range(20)]
+    run(*setup(1, 8, 4, 128, 16, "bf16", ctx, 311), ctx, 311, "bf16")
+
+
 def test_full_batch():
-    ctx = [48 + (i % 5) for i in range(256)]
-    run(*setup(1, 1, 2, 64, 16, "bf16", ctx, 3), ctx, 3, "bf16")
+    ctx = [304 + (i % 5) for i in range(256)]
+    run(*setup(1, 8, 1, 64, 16, "bf16", ctx, 19), ctx, 19, "bf16", once=True)
+
+
+# the batch of the tests below, and its prefix: rows of both halves of a product's
+# columns, three tiles, the last one partly filled
+CTX, PREFIX = [688 + (5 * i) % 13 for i in range(30)], 43
+SHAPE = (1, 16, 1, 128, 16)
 
 
 @pytest.mark.parametrize("scale", [-0.2, 0.0, 3.0])
 def test_other_scales(scale):
     """A negative scale turns the order of the scores round, a large one makes
     one weight outweigh all others, and its partition's maximum move."""
-    ctx = [600, 577, 592]
-    run(*setup(1, 2, 4, 128, 16, "bf16", ctx, 36), ctx, 36, "bf16", scale=scale)
+    run(*setup(*SHAPE, "bf16", CTX, PREFIX), CTX, PREFIX, "bf16", scale=scale, once=True)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
-def test_rising_scores(dtype):
+@pytest.mark.parametrize("step", [0.5, 5.0, 30.0])
+def test_rising_scores(dtype, step):
     """Scores that rise token by token by less than, and by more than, what the
     running maximum lets pass."""
-    for step in (0.5, 5.0, 30.0):
-        ctx = [257, 300]
-        kv, q, tables = setup(1, 1, 2, 64, 16, dtype, ctx, 16)
-        q[:] = 0
-        q[..., 0] = 1
-        for b in range(2):
-            blk, slot = oc.rows_of(tables, b, range(ctx[b]), 16)
-            kv[0, 0, blk, slot, 0, 0] = (torch.arange(ctx[b]) * step / 8).to(kv.dtype)
-        run(kv, q, tables, ctx, 16, dtype, scale=1.0)
+    kv, q, tables = setup(*SHAPE, dtype, CTX, PREFIX)
+    q[:] = 0
+    q[..., 0] = 1
+    for b in range(len(CTX)):
+        blk, slot = oc.rows_of(tables, b, range(CTX[b]), 16)
+        kv[0, 0, blk, slot, :, 0] = (torch.arange(CTX[b]) * step / 8).to(kv.dtype)[:, None]
+    run(kv, q, tables, CTX, PREFIX, dtype, scale=1.0, once=True)
 
 
 @pytest.mark.parametrize("where", ["prefix", "own"])
 @pytest.mark.parametrize("bad", ["nan", "inf", "-inf", "all -inf"])
 def test_nonfinite_scores(where, bad):
-    """A NaN or +inf score gives that row zeros and no other; -inf a weight of 0."""
-    ctx = [200, 192, 210]
-    kv, q, tables = setup(1, 2, 2, 128, 16, "bf16", ctx, 12)
+    """A NaN or +inf score gives its rows zeros and no others; -inf is a weight
+    of 0.  Head 1 alone has such keys, in the prefix or in sequence 2's own
+    tokens."""
+    kv, q, tables = setup(*SHAPE, "bf16", CTX, PREFIX)
     q[..., 0], kv[0, ..., 0] = 4.0, 0.0
-    tokens = range(0, 192) if where == "prefix" else range(192, ctx[0])
+    tokens = range(0, 688) if where == "prefix" else range(688, CTX[2])
     if bad != "all -inf":
         tokens = [tokens[3], tokens[5]]
-    blk, slot = oc.rows_of(tables, 0, tokens, 16)
-    # the value's product with q overflows in 32 bits, or does not need to
+    blk, slot = oc.rows_of(tables, 2, tokens, 16)
     kv[0, 0, blk, slot, 1, 0] = {"nan": float("nan"), "inf": float("inf")}.get(bad, float("-inf"))
-    out = run(kv, q, tables, ctx, 12, "bf16")
+    out = run(kv, q, tables, CTX, PREFIX, "bf16", once=True)
     if bad in ("nan", "inf"):
-        assert bool((out[0, 0, 2:] == 0).all()) and bool((out[0, 0, :2] != 0).any())
+        hit = range(len(CTX)) if where == "prefix" else [2]
+        for b in range(len(CTX)):
+            assert bool((out[0, b, 1] == 0).all()) == (b in hit)
+        assert bool((out[0, :, 0] != 0).any(-1).all())
 
 
 def test_what_lies_behind_a_sequence_does_not_count():
     """Slots behind the last token, and blocks of others, may hold NaN."""
-    ctx = [100, 97, 96]
-    kv, q, tables = setup(1, 2, 2, 128, 16, "bf16", ctx, 6)
-    used = torch.zeros(kv.shape[2:4], dtype=torch.bool)
-    for b, n in enumerate(ctx):
-        used[oc.rows_of(tables, b, range(n), 16)] = True
-    kv[:, :, ~used] = float("nan")
-    run(kv, q, tables, ctx, 6, "bf16")
+    for shape, ctx, prefix in ((SHAPE, CTX, PREFIX), ((1, 2, 2, 128, 16), [100, 97, 96], 6)):
+        kv, q, tables = setup(*shape, "bf16", ctx, prefix)
+        used = torch.zeros(kv.shape[2:4], dtype=torch.bool)
+        for b, n in enumerate(ctx):
+            used[oc.rows_of(tables, b, range(n), 16)] = True
+        kv[:, :, ~used] = float("nan")
+        run(kv, q, tables, ctx, prefix, "bf16")
 
 
 def test_on_a_stream_replayed_and_repeated():
     """Captured once and replayed, with eager calls between, every result has
     the same bits; the same call on two streams with workspaces of their own, too."""
-    ctx, prefix = [700, 643, 640, 901], 40
-    kv, q, tables = setup(2, 2, 4, 128, 16, "bf16", ctx, prefix)
-    first = run(kv, q, tables, ctx, prefix, "bf16")
+    ctx, prefix = CTX, PREFIX
+    kv, q, tables = setup(*SHAPE, "bf16", ctx, prefix)
+    first = run(kv, q, tables, ctx, prefix, "bf16", once=True)
     dev = kv.cuda()
     pool = Pool(list(dev[0].unbind(0)), list(dev[1].unbind(0)))
     nbytes = decode_prefix_workspace_bytes(pool, ctx, q.shape[2], prefix)
