@@ -145,11 +145,39 @@ __device__ __forceinline__ uint64_t score_key(double x)
     return u >> 63 ? ~u : u | 1ull << 63;
 }
 
+// x of another lane of the row of 16 (DPP control CTRL).
+template <int CTRL>
+__device__ __forceinline__ double of_lane(double x)
+{
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    const i32x2 v = __builtin_bit_cast(i32x2, x);
+    return __builtin_bit_cast(double, i32x2{__builtin_amdgcn_update_dpp(0, v.x, CTRL, 0xf, 0xf, false),
+                                            __builtin_amdgcn_update_dpp(0, v.y, CTRL, 0xf, 0xf, false)});
+}
+
+constexpr int kLaneXor1 = 0xB1, kLaneXor2 = 0x4E, kLaneXor7 = 0x141, kLaneXor8 = 0x128;
+
+// The sums over C lanes (8 or 16, a head's) of four values: lane c gets that of
+// value c / (C / 4).  Lanes l and l ^ mask exchange what the other keeps, then the
+// few lanes of each value add up.  Each value's sum is the same tree, so equal
+// values give equal sums.
+template <uint32_t C>
+__device__ __forceinline__ double sums_of_four(const double *s, uint32_t c)
+{
+    constexpr int kFirst = C == 16 ? kLaneXor8 : kLaneXor7, kSecond = C == 16 ? kLaneXor7 : kLaneXor2;
+    const bool upper = c & (C / 2), odd = c & (C / 4);
+    const double a = (upper ? s[2] : s[0]) + of_lane<kFirst>(upper ? s[0] : s[2]);
+    const double b = (upper ? s[3] : s[1]) + of_lane<kFirst>(upper ? s[1] : s[3]);
+    double x = (odd ? b : a) + of_lane<kSecond>(odd ? a : b);
+    if constexpr (C == 16)
+        x += of_lane<kLaneXor2>(x);
+    return x + of_lane<kLaneXor1>(x);
+}
+
 // A lane takes 8 dims of one KV head, its sums P and N in registers, over the
-// consecutive blocks of its row of lanes, kScoreAhead blocks' bounds in flight;
-// the D / 8 lanes of a head add up, and each keeps the score of one block in
-// D / 8, so that scores leave as whole lines.
-constexpr uint32_t kScoreAhead = 4;
+// consecutive blocks of its row of lanes, four blocks' bounds in flight; the D / 8
+// lanes of a head add up, and each keeps the score of one block in D / 8, so that
+// scores leave as whole lines.
 
 template <int BF16, int D>
 __global__ void __launch_bounds__(kThreads) score_blocks(const SelectArgs a)
@@ -176,60 +204,92 @@ __global__ void __launch_bounds__(kThreads) score_blocks(const SelectArgs a)
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         p[e] = m[e] = 0.0;
-    for (uint32_t h = 0; h < G; ++h) {
-        float x[8];
-        unpack8<BF16>(load16(a.q + (((static_cast<uint64_t>(layer) * a.batch + s) * a.q_heads + head * G + h) * C + c) * 16u), x);
+    const uint8_t *q = a.q + (((static_cast<uint64_t>(layer) * a.batch + s) * a.q_heads + head * G) * C + c) * 16u;
+    for (uint32_t h0 = 0; h0 < G; h0 += 4u) {
+        u32x4 x[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            p[e] += x[e] < 0.f ? 0.0 : static_cast<double>(x[e]);
-            m[e] += x[e] > 0.f ? 0.0 : static_cast<double>(x[e]);
+        for (uint32_t u = 0; u < 4u; ++u)
+            x[u] = load16(q + min(h0 + u, G - 1u) * C * 16u);
+#pragma unroll
+        for (uint32_t u = 0; u < 4u; ++u) {
+            float f[8];
+            unpack8<BF16>(x[u], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = h0 + u < G ? f[e] : 0.f;
+                p[e] += static_cast<double>(v < 0.f ? 0.f : v);
+                m[e] += static_cast<double>(v > 0.f ? 0.f : v);
+            }
         }
     }
     const uint8_t *lo = reinterpret_cast<const uint8_t *>(table_entry(a.tab, layer));
     const uint8_t *hi = reinterpret_cast<const uint8_t *>(table_entry(a.tab, a.num_layers + layer));
     const uint32_t j0 = (part * rows + (in ? r : 0u)) * a.per_row;
     uint64_t *out = a.keys + key_row(a, layer, first, n, head);
-    uint64_t kept = 0;
-    for (uint32_t k0 = 0; k0 < a.per_row; k0 += kScoreAhead) {
-        u32x4 x[kScoreAhead], y[kScoreAhead];
+    // bounds of four blocks, and the ids of the four after them
+    u32x4 x[4], y[4];
+    uint32_t ids[4];
+    auto look_up = [&](uint32_t k0) {
 #pragma unroll
-        for (uint32_t u = 0; u < kScoreAhead; ++u) {
-            const uint32_t j = min(j0 + k0 + u, n - 1u);
-            const uint32_t id = min(table_id(a.tables, s, a.table_stride, j), a.num_blocks - 1u);
-            const uint64_t at = (static_cast<uint64_t>(id) * row + (in ? chunk : 0u)) * 16u;
+        for (uint32_t u = 0; u < 4u; ++u)
+            ids[u] = table_id(a.tables, s, a.table_stride, min(j0 + k0 + u, n - 1u));
+    };
+    auto fetch = [&]() {
+#pragma unroll
+        for (uint32_t u = 0; u < 4u; ++u) {
+            const uint64_t at = (static_cast<uint64_t>(min(ids[u], a.num_blocks - 1u)) * row + (in ? chunk : 0u)) * 16u;
             x[u] = load16(hi + at);
             y[u] = load16(lo + at);
         }
+    };
+    look_up(0);
+    fetch();
+    look_up(4);
+    uint64_t kept = 0;
+    for (uint32_t k0 = 0; k0 < a.per_row; k0 += 4u) {
+        u32x4 up4[4], low4[4];
 #pragma unroll
-        for (uint32_t u = 0; u < kScoreAhead; ++u) {
+        for (uint32_t u = 0; u < 4u; ++u) {
+            up4[u] = x[u];
+            low4[u] = y[u];
+        }
+        if (k0 + 4u < a.per_row) {
+            fetch();
+            look_up(k0 + 8u);
+        }
+        double sum[4];
+#pragma unroll
+        for (uint32_t u = 0; u < 4u; ++u) {
             float up[8], low[8];
-            unpack8<BF16>(x[u], up);
-            unpack8<BF16>(y[u], low);
-            double sum = 0.0;
+            unpack8<BF16>(up4[u], up);
+            unpack8<BF16>(low4[u], low);
+            sum[u] = 0.0;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                sum += p[e] * static_cast<double>(up[e]) + m[e] * static_cast<double>(low[e]);
-#pragma unroll
-            for (uint32_t d = 1; d < C; d *= 2)
-                sum += __shfl_xor(sum, d);
-            if (c == (k0 + u) % C)
-                kept = score_key(sum);
+                sum[u] += p[e] * static_cast<double>(up[e]) + m[e] * static_cast<double>(low[e]);
         }
-        const uint32_t done = k0 + kScoreAhead;             // per_row is a multiple of C, or less than C
+        // lane c has the score of block k0 + c / (C / 4); every C blocks, or at the
+        // end, the lanes that share one take it for different k0
+        const double score = sums_of_four<C>(sum, c);
+        const uint32_t mine = c % (C / 4) * 4u + c / (C / 4);
+        if (c % (C / 4) == k0 / 4u % (C / 4))
+            kept = score_key(score);
+        const uint32_t done = k0 + 4u;             // per_row is a multiple of C, or less than C
         if (done % C == 0 || done >= a.per_row) {
-            const uint32_t j = j0 + (done - 1u) / C * C + c;
-            if (in && j < j0 + min(done, a.per_row) && j < n)
+            const uint32_t k = (done - 1u) / C * C + mine, j = j0 + k;
+            if (in && k < done && j < n)
                 out[j] = kept;
         }
     }
 }
 
-// Blocks of a row of lanes, for `work` rows of lanes times blocks in all:
-// enough workgroups to fill the chip before a row of lanes takes more than it
-// can have in flight.
+// Blocks of a row of lanes, for `work` rows of lanes times blocks in all: more of
+// them share the setup (the sums of the queries), if enough workgroups are left to
+// fill the chip.  12 requests of up to 65536 tokens, 4 layers of 8 heads, 8 / 16 / 32
+// blocks 81 / 68 / 69 us; 16 of up to 32000, one layer, 19.5 / 19.5 / 19.2.
 inline uint32_t score_blocks_per_row(uint64_t work)
 {
-    return work >= 16 * 2048 ? 16 : work >= 8 * 1024 ? 8 : 4;
+    return work >= 16 * 1024 ? 16 : work >= 8 * 512 ? 8 : 4;
 }
 
 // The parallel part of a pass of the search below: of the counts of 256 bins,
@@ -340,8 +400,23 @@ __global__ void __launch_bounds__(T) list_blocks(const SelectArgs a)
     bool ties = true;                  // whether not all of them are
     for (; shift >= 0 && ties; shift -= 8) {
         each([&](uint32_t j, uint64_t k) {
-            if (j < n && (shift == 56 || k >> (shift + 8) == prefix))
-                atomicAdd(&bins[static_cast<uint32_t>(k >> shift) & 255u], 1u);
+            const bool counts = j < n && (shift == 56 || k >> (shift + 8) == prefix);
+            const uint32_t bin = static_cast<uint32_t>(k >> shift) & 255u;
+            if (shift == 56) {       // sign and exponent: the keys of a wavefront mostly share a bin
+                const uint64_t left = __ballot(counts);
+                if (!left)
+                    return;
+                const uint32_t first_lane = __ffsll(static_cast<unsigned long long>(left)) - 1;
+                const uint32_t common = __builtin_amdgcn_readlane(bin, first_lane);
+                const uint64_t alike = __ballot(counts && bin == common);
+                if (lane == first_lane)
+                    atomicAdd(&bins[common], static_cast<uint32_t>(__popcll(alike)));
+                else if (counts && bin != common)
+                    atomicAdd(&bins[bin], 1u);
+                return;
+            }
+            if (counts)
+                atomicAdd(&bins[bin], 1u);
         });
         __syncthreads();
         find_bin(bins, wave_sum, found, need);
@@ -424,12 +499,14 @@ __global__ void __launch_bounds__(T) list_blocks(const SelectArgs a)
     }
 }
 
-// The kernel for rows of at most `longest` blocks, and its threads.
+// The kernel for rows of at most `longest` blocks, and its threads.  384 rows of up
+// to 4096 blocks, 256 / 512 / 1024 threads 16.4 / 12.4 / 11.9 us; 24 of up to 563 take
+// 5.6 with 256.
 inline const void *list_kernel(uint32_t longest, uint32_t *threads)
 {
-    *threads = longest <= 4096 ? 256 : 1024;
+    *threads = longest <= 1024 ? 256 : 1024;
     return longest <= 1024    ? reinterpret_cast<const void *>(&list_blocks<256, 4>)
-           : longest <= 4096  ? reinterpret_cast<const void *>(&list_blocks<256, 16>)
+           : longest <= 4096  ? reinterpret_cast<const void *>(&list_blocks<1024, 4>)
            : longest <= 16384 ? reinterpret_cast<const void *>(&list_blocks<1024, 16>)
                               : reinterpret_cast<const void *>(&list_blocks<1024, 0>);
 }

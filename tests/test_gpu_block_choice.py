@@ -115,7 +115,7 @@ def random_bounds(kv, gen):
     (2, 3, 1, 64, 8, [500, 77, 400], 0, 0, 7), (1, 1, 16, 128, 4, [1500], 2, 3, 5), (1, 40, 1, 128, 16, [300], 0, 1, 3),
     (1, 13, 2, 64, 16, [900, 899], 0, 0, 56), (1, 1, 1, 64, 1, [3000, 2999, 257], 1, 2, 100),
     (1, 2, 2, 128, 16, [4000], 0, 0, 249), (1, 2, 2, 128, 16, [4000], 0, 0, 250), (1, 2, 2, 128, 16, [4000], 0, 0, 500),
-    (1, 1, 2, 64, 2, [20000], 4, 4, 1000)])
+    (1, 1, 2, 64, 2, [20000], 4, 4, 1000), (1, 1, 1, 64, 1, [17000, 16385, 40], 2, 3, 300)])
 def test_choice(dtype, L, H, G, D, bs, ctx, first, last, count):
     print("[case]", L, H, G, D, bs, ctx, first, last, count, flush=True)
     kv, q, tables, gen = make(L, H, G, D, bs, dtype, ctx)
@@ -130,6 +130,15 @@ def test_equal_scores_go_to_the_first():
     for count in (1, 10, 40, 99):
         choose(b, q, tables, [1600], 16, 0, 0, count)
         choose(b, q, tables, [1600], 16, 0, 1, count)
+
+
+@pytest.mark.parametrize("blocks", [5000, 17000])
+def test_equal_scores_of_long_rows(blocks):
+    kv, q, tables, gen = make(1, 1, 1, 64, 1, "fp16", [blocks])
+    b = random_bounds(kv, gen)
+    b = b[:, :, torch.arange(b.shape[2]) % 7]
+    for count in (600, 3000):
+        choose(b, q, tables, [blocks], 1, 1, 2, count)
 
 
 def test_scores_that_differ_by_little():

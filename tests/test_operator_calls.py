@@ -110,7 +110,7 @@ def test_select_scores_only_what_has_to_be_chosen_from(call):
         dict(op="select", ctx_lens=[16 * 1025, 3], table_stride=2000), dict(op="select", ctx_lens=[16 * 4097, 3], table_stride=9000),
         dict(op="select", ctx_lens=[16 * 16385, 3], table_stride=20000)])
     assert kernels(few) == ["list_blocks"] and kernels(many) == ["score_blocks", "list_blocks"]
-    assert [x["launches"][-1]["template"] for x in (many, long, longer, longest)] == [[256, 4], [256, 16], [1024, 16],
+    assert [x["launches"][-1]["template"] for x in (many, long, longer, longest)] == [[256, 4], [1024, 4], [1024, 16],
                                                                                       [1024, 0]]
 
 
