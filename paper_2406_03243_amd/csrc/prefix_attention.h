@@ -18,13 +18,7 @@
 
 namespace {
 
-// Tokens of K and V in LDS at a time, for wm wavefronts along the rows: few rows
-// wait for memory and want much of it in flight, many for the matrix cores and
-// want the registers.
-constexpr uint32_t prefix_tile(uint32_t wm)
-{
-    return wm >= 2 ? 64 : 128;
-}
+constexpr uint32_t kPrefixTile = 64;      // tokens of K and V in LDS at a time
 
 struct PrefixArgs {
     const uint64_t *tab;         // pool table: K bases then V bases
@@ -34,7 +28,7 @@ struct PrefixArgs {
     float scale;
     uint32_t num_layers, batch, q_heads, kv_heads, num_blocks, block_size;
     uint32_t tokens;             // of the prefix
-    uint32_t part_tokens, parts; // a partition's tokens (a multiple of its tile), partitions
+    uint32_t part_tokens, parts; // a partition's tokens (a multiple of kPrefixTile), partitions
     uint32_t members;            // sequences behind the prefix
     uint32_t chunks;             // workgroups that share a partition's rows
     Divisor by_block;
@@ -112,15 +106,16 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
     constexpr uint32_t LPR = D / 8;                // 16-byte chunks of a row
     constexpr uint32_t RB = D * 2;                 // bytes of a row
     constexpr uint32_t RPB = 128 / D;              // rows per 256 bytes
-    constexpr uint32_t T = prefix_tile(WM), BUFS = T == 64 ? 2 : 1;
+    constexpr uint32_t T = kPrefixTile;
     constexpr int STEPS = T * WM / 128;            // of 32 tokens a wavefront takes of a tile
     constexpr int CPT = T * LPR / kThreads;    // chunks of K, and of V, a thread brings per tile
     constexpr uint32_t RPI = kThreads / LPR;       // rows that the threads bring at a time
     constexpr float kLog2e = 1.4426950408889634f;
     constexpr uint32_t kTileBytes = T * RB;
-    constexpr uint32_t kMergeRow = D + 4;
-    __shared__ __align__(16) uint8_t smem[BUFS][2][kTileBytes];   // K, V
-    static_assert(4 * 16 * kMergeRow * 4 <= 2 * BUFS * kTileBytes, "the merge of 16 rows fits");
+    // Two tiles, K and V, the one in work and the one on its way: arrays of their
+    // own, so that the compiler sees which loads a read has to wait for.
+    __shared__ __align__(16) uint8_t tile_a[2 * kTileBytes], tile_b[2 * kTileBytes];
+    static_assert(4 * 16 * D * 4 <= 2 * kTileBytes, "the merge of 16 rows fits");
     __shared__ float sh_m[4][32], sh_l[4][32];
 
     // The workgroups that read the same tokens (a partition's row chunks, then
@@ -158,12 +153,16 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
             qf[ks] = load16(a.q + (q_row * D + 16 * ks + 8 * half) * 2) ^ sign;
     }
 
-    // A tile's rows: the thread's chunk of token th + i * RPI, brought into
-    // registers while the tile before it is worked on, and their blocks' ids one
-    // tile ahead of them.  Past the partition's end valid rows repeat; they
-    // weigh 0.
+    // A tile's rows go from memory straight into LDS: load i of a thread brings 16
+    // bytes of token th + i * RPI while the tile before is worked on, and the ids of
+    // the blocks are looked up one tile ahead of that.  Past the partition's end
+    // valid rows repeat; they weigh 0.  Slot c of token t in LDS takes the row's
+    // 16-byte chunk c ^ swizzle(t), so that what is read at once falls on distinct
+    // banks: of K a chunk of each of 16 rows, of V four chunks of each of 4 rows.
+    auto k_swizzle = [](uint32_t t) { return (t / RPB) % LPR; };
+    auto v_swizzle = [](uint32_t t) { return t / RPB % (4u / RPB) * 4u ^ t / 4u % 4u; };
+    static_assert(RPI % 16 == 0, "a thread's rows swizzle alike");
     const uint32_t th = threadIdx.x / LPR, tc = threadIdx.x % LPR;
-    u32x4 kr[CPT], vr[CPT];
     uint32_t ids[CPT];
     // ALIGNED: the first of the 16 tokens (t_end is a multiple of 16) to which the
     // wavefront's rows of load i belong; else the thread's token.
@@ -171,7 +170,8 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
     auto token_of = [&](uint32_t t0, uint32_t i) {
         return ALIGNED ? min(t0 + (i * RPI + wave_row) / 16u * 16u, t_end - 16u) : min(t0 + i * RPI + th, t_end - 1u);
     };
-    const uint64_t lane_at = (ALIGNED ? static_cast<uint64_t>(th % 16u) * a.kv_heads * RB : 0u) + 16u * tc;
+    const uint64_t lane_row = ALIGNED ? static_cast<uint64_t>(th % 16u) * a.kv_heads * RB : 0u;
+    const uint8_t *k_lane = kbase + lane_row + 16u * (tc ^ k_swizzle(th)), *v_lane = vbase + lane_row + 16u * (tc ^ v_swizzle(th));
     auto look_up = [&](uint32_t t0) {
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
@@ -179,28 +179,16 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
             ids[i] = ALIGNED ? static_cast<uint32_t>(id_entry(a.table, uniform(blk))) : static_cast<uint32_t>(a.table[blk]);
         }
     };
-    auto fetch = [&](uint32_t t0) {
+    auto fetch = [&](uint8_t *tile, uint32_t t0) {
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
             const uint32_t t = token_of(t0, i), blk = divide(t, a.by_block);
             const uint64_t slot = static_cast<uint64_t>(min(ids[i], a.num_blocks - 1u)) * a.block_size + (t - blk * a.block_size);
-            const uint64_t at = (slot * a.kv_heads + g) * RB + lane_at;
-            kr[i] = *(const LLMIG_GLOBAL u32x4 *)(kbase + at);
-            vr[i] = *(const LLMIG_GLOBAL u32x4 *)(vbase + at);
-        }
-    };
-    // 16-byte chunk c of token t sits at chunk c ^ swizzle(t) of its row, so that
-    // what is read at once falls on distinct banks: of K a chunk of each of 16
-    // rows, of V four chunks of each of 4 rows.
-    auto k_swizzle = [](uint32_t t) { return (t / RPB) % LPR; };
-    auto v_swizzle = [](uint32_t t) { return t / RPB % (4u / RPB) * 4u ^ t / 4u % 4u; };
-    static_assert(RPI % 16 == 0, "a thread's rows swizzle alike");
-    const uint32_t put_k = th * RB + 16u * (tc ^ k_swizzle(th)), put_v = th * RB + 16u * (tc ^ v_swizzle(th));
-    auto put = [&](uint32_t buf) {
-#pragma unroll
-        for (int i = 0; i < CPT; ++i) {
-            *reinterpret_cast<u32x4 *>(&smem[buf][0][put_k + i * RPI * RB]) = kr[i];
-            *reinterpret_cast<u32x4 *>(&smem[buf][1][put_v + i * RPI * RB]) = vr[i];
+            const uint64_t at = (slot * a.kv_heads + g) * RB;
+            uint8_t *to = tile + (i * RPI + wave_row) * RB;
+            __builtin_amdgcn_global_load_lds((const void LLMIG_GLOBAL *)(k_lane + at), (void LLMIG_LDS *)to, 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const void LLMIG_GLOBAL *)(v_lane + at), (void LLMIG_LDS *)(to + kTileBytes), 16,
+                                             0, 0);
         }
     };
 
@@ -223,9 +211,9 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
             acc[mt][i] = 0.f;
 
     // A tile in LDS; TAIL: the partition ends in it.
-    auto work = [&](uint32_t buf, uint32_t t0, auto tail_c) {
+    auto work = [&](const uint8_t *tile, uint32_t t0, auto tail_c) {
         constexpr bool TAIL = decltype(tail_c)::value;
-        const uint8_t *kt = smem[buf][0] + wt * (32u * STEPS) * RB, *vt = smem[buf][1] + wt * (32u * STEPS) * RB;
+        const uint8_t *kt = tile + wt * (32u * STEPS) * RB, *vt = kt + kTileBytes;
         auto k_rows = [&](int step, int ks) {
             return *reinterpret_cast<const u32x4 *>(kt + 32 * step * RB + k_at + (k_x ^ (32u * ks)));
         };
@@ -326,37 +314,35 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
         }
     };
 
-    look_up(t_begin);
-    fetch(t_begin);
-    look_up(t_begin + T);
-    uint32_t t0 = t_begin, buf = 0;
-    if constexpr (BUFS == 2)
-        put(0);
-    for (; t0 + T <= t_end; t0 += T) {
-        __syncthreads();                      // the tile before it is done with
-        if constexpr (BUFS == 1) {
-            put(0);
-            __syncthreads();
-        }
-        const bool more = t0 + T < t_end;
-        if (more) {
-            fetch(t0 + T);
+    // A whole tile: every thread's part of it has landed, the tile after it is
+    // requested, then the work.
+    auto landed = [&]() {
+        __builtin_amdgcn_s_waitcnt(kWaitVm0);
+        __syncthreads();
+    };
+    auto turn = [&](const uint8_t *tile, uint8_t *next, uint32_t t0) {
+        landed();
+        if (t0 + T < t_end) {
+            fetch(next, t0 + T);
             look_up(t0 + 2 * T);
         }
-        work(buf, t0, std::false_type());
-        if constexpr (BUFS == 2) {
-            buf ^= 1u;
-            if (more)
-                put(buf);
-        }
+        work(tile, t0, std::false_type());
+    };
+    look_up(t_begin);
+    fetch(tile_a, t_begin);
+    look_up(t_begin + T);
+    uint32_t t0 = t_begin;
+    for (; t0 + 2 * T <= t_end; t0 += 2 * T) {
+        turn(tile_a, tile_b, t0);
+        turn(tile_b, tile_a, t0 + T);
+    }
+    if (t0 + T <= t_end) {
+        turn(tile_a, tile_b, t0);
+        t0 += T;
     }
     if (t0 < t_end) {
-        __syncthreads();
-        if constexpr (BUFS == 1) {
-            put(0);
-            __syncthreads();
-        }
-        work(buf, t0, std::true_type());
+        landed();
+        work((t0 - t_begin) / T % 2u ? tile_b : tile_a, t0, std::true_type());
     }
 
     // The wavefronts that split the tokens meet in LDS, 16 rows of each at a
@@ -366,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
         sh_m[wave][l32] = m;
         sh_l[wave][l32] = lsum;
     }
-    float *so = reinterpret_cast<float *>(&smem[0][0][0]);         // [wave][16 rows][kMergeRow]
+    float *so = reinterpret_cast<float *>(tile_a);                // [wave][16 rows][D]
 #pragma unroll
     for (uint32_t rt = 0; rt < 2; ++rt) {
         __syncthreads();
@@ -375,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    *reinterpret_cast<f32x4_t *>(so + (wave * 16u + r16) * kMergeRow + 32 * mt + 8 * i + 4 * half) =
+                    *reinterpret_cast<f32x4_t *>(so + (wave * 16u + r16) * D + 32 * mt + 8 * i + 4 * half) =
                         f32x4_t{acc[mt][4 * i], acc[mt][4 * i + 1], acc[mt][4 * i + 2], acc[mt][4 * i + 3]};
         }
         __syncthreads();
@@ -396,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
                 // (no weight: a factor of 1 would do as well, but for a NaN sum)
                 const float c = mw == -INFINITY ? 1.f : exp2f(mw - mm);
                 ll += sh_l[v][16 * rt + rr] * c;
-                o += *reinterpret_cast<const f32x4_t *>(so + (v * 16u + rr) * kMergeRow + 4 * d4) * c;
+                o += *reinterpret_cast<const f32x4_t *>(so + (v * 16u + rr) * D + 4 * d4) * c;
             }
             float *rec = a.ws + (((static_cast<uint64_t>(layer) * a.parts + part) * a.members + row / G) * a.q_heads + g * G +
                                  row % G) * (D + kAttnHeader);
@@ -492,9 +478,8 @@ inline const void *prefix_join_kernel(int head_dim, uint64_t rows, uint32_t most
 template <int BF16, int D, int ALIGNED>
 const void *prefix_kernel(uint32_t wm)
 {
-    return wm == 1   ? reinterpret_cast<const void *>(&prefix_rows<BF16, D, 1, ALIGNED>)
-           : wm == 2 ? reinterpret_cast<const void *>(&prefix_rows<BF16, D, 2, ALIGNED>)
-                     : reinterpret_cast<const void *>(&prefix_rows<BF16, D, 4, ALIGNED>);
+    return wm == 2 ? reinterpret_cast<const void *>(&prefix_rows<BF16, D, 2, ALIGNED>)
+                   : reinterpret_cast<const void *>(&prefix_rows<BF16, D, 4, ALIGNED>);
 }
 
 template <int BF16, int D>
@@ -540,10 +525,10 @@ inline int64_t prefix_cut_ns(int64_t workgroups, int64_t tiles, int64_t records,
 inline PrefixCut prefix_cut(uint32_t rows, int64_t tokens, int64_t layer_heads, int64_t head_dim)
 {
     PrefixCut c;
-    c.wm = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+    c.wm = rows <= 64 ? 2 : 4;
     c.chunks = (rows + 32 * c.wm - 1) / (32 * c.wm);
     c.ns = -1;
-    const uint32_t tile = prefix_tile(c.wm);
+    constexpr uint32_t tile = kPrefixTile;
     const int64_t tiles = (tokens + tile - 1) / tile, most = std::min<int64_t>(tiles, kPrefixMostParts);
     for (int64_t want = 1; want <= most; ++want) {
         const int64_t per = (tiles + want - 1) / want, parts = (tiles + per - 1) / per;
