@@ -219,7 +219,7 @@ class Pool:
         handle = _vp()
         _check(_lib.llmig_pool_create(ctypes.byref(desc), ctypes.byref(handle)), "llmig_pool_create")
         self._handle = handle
-        self.k, self.v = list(k_layers), list(v_layers)
+        self.k, self.v, self.dtype = list(k_layers), list(v_layers), t0.dtype
         self.num_layers, self.num_blocks, self.block_size = len(k_layers), nb, bs
         self.num_kv_heads, self.head_dim, self.elem_bytes = heads, dim, t0.element_size()
         self.layouts = (int(layouts[0]), int(layouts[1]))
@@ -575,16 +575,17 @@ def _workspace(workspace: torch.Tensor) -> int:
     return workspace.nbytes
 
 
-def _token_rows(t: torch.Tensor, pool: Pool, tokens: int, heads: int, name: str):
-    """Checks [L][tokens][heads][D] rows of new tokens; returns their layer and
-    token strides (0 along an axis of one entry, whose stride may be any)."""
-    layers, dim = pool.num_layers, pool.head_dim
-    if not t.is_cuda or t.dtype != pool.k[0].dtype or t.shape != (layers, tokens, heads, dim):
+def _token_rows(t: torch.Tensor, dtype, shape, name: str):
+    """Checks rows of new tokens, [L][tokens][heads][D]; returns their address,
+    layer and token strides (0 along an axis of one entry, whose stride may be
+    any)."""
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA [layers][tokens][heads][head_dim] tensor of the pool's type")
+    layers, tokens, heads, dim = shape
     layer, token, head, one = t.stride()
-    if tokens and ((one != 1 and dim > 1) or (head != dim and heads > 1)):
+    if (one != 1 and dim > 1) or (head != dim and heads > 1):
         raise ValueError(f"the heads of a token of {name} must be contiguous")
-    return layer if layers > 1 else 0, token if tokens > 1 else 0
+    return t.data_ptr(), layer if layers > 1 else 0, token if tokens > 1 else 0
 
 
 def llmig_append_rotary(pool: Pool, k: torch.Tensor, v: torch.Tensor, tables: torch.Tensor, from_toks, n_toks,
@@ -599,35 +600,42 @@ def llmig_append_rotary(pool: Pool, k: torch.Tensor, v: torch.Tensor, tables: to
     output).  cos_sin: CUDA float32 [positions][rotary_dim], cosines then
     sines (None: no rotation).  first_pos: positions of the first new tokens
     (default: from_toks)."""
-    code = _type_code(pool.k[0].dtype, "the pool")
+    dtype = pool.dtype
+    code = _type_code(dtype, "the pool")
     fp, batch, f = _lens(from_toks)
     np_, count, n = _lens(n_toks)
-    pp = p = None
+    pp = 0
     if first_pos is not None:
         pp, places, p = _lens(first_pos)
-    if count != batch or (p is not None and places != batch):
-        raise ValueError("from_toks, n_toks and first_pos must hold one number per sequence")
+        if places != batch:
+            raise ValueError("first_pos must hold one position per sequence")
+    if count != batch:
+        raise ValueError("from_toks and n_toks must hold one number per sequence")
     total = sum(n) if type(n) is array else int(n.sum(dtype=np.int64))
-    k_at, v_at = _token_rows(k, pool, total, pool.num_kv_heads, "k"), _token_rows(v, pool, total, pool.num_kv_heads, "v")
-    q_heads, q_at = 0, (0, 0)
-    if (q is None) != (q_out is None):
-        raise ValueError("q and q_out come together")
+    layers, dim = pool.num_layers, pool.head_dim
+    shape = (layers, total, pool.num_kv_heads, dim)
+    kp, k_layer, k_token = _token_rows(k, dtype, shape, "k")
+    vp, v_layer, v_token = _token_rows(v, dtype, shape, "v")
+    qp = op = q_heads = q_layer = q_token = 0
     if q is not None:
-        if q.dim() != 4:
-            raise ValueError("q must be a [layers][tokens][heads][head_dim] tensor")
+        if q.dim() != 4 or q_out is None:
+            raise ValueError("q must be a [layers][tokens][heads][head_dim] tensor and come with q_out")
         q_heads = q.shape[2]
-        q_at = _token_rows(q, pool, total, q_heads, "q")
-        if q_out.shape != q.shape or q_out.dtype != q.dtype or not q_out.is_cuda or not q_out.is_contiguous():
+        qp, q_layer, q_token = _token_rows(q, dtype, (layers, total, q_heads, dim), "q")
+        if q_out.shape != q.shape or q_out.dtype is not dtype or not q_out.is_cuda or not q_out.is_contiguous():
             raise ValueError("q_out must be a contiguous CUDA tensor of q's shape and type")
+        op = q_out.data_ptr()
+    elif q_out is not None:
+        raise ValueError("q and q_out come together")
     stride = _device_tables(tables, batch)
-    positions = rotary = 0
+    cp = positions = rotary = 0
     if cos_sin is not None:
-        if cos_sin.dtype != torch.float32 or not cos_sin.is_cuda or not cos_sin.is_contiguous() or cos_sin.dim() != 2:
+        if cos_sin.dtype is not torch.float32 or not cos_sin.is_cuda or not cos_sin.is_contiguous() or cos_sin.dim() != 2:
             raise ValueError("cos_sin must be a contiguous CUDA float32 [positions][rotary_dim] tensor")
         positions, rotary = cos_sin.shape
-    d = _append_desc.pack(code, batch, q_heads, stride, q.data_ptr() if q_heads else 0, k.data_ptr(), v.data_ptr(),
-                          q_out.data_ptr() if q_heads else 0, *q_at, *k_at, *v_at, tables.data_ptr(), fp, np_, pp or 0,
-                          cos_sin.data_ptr() if rotary else 0, positions, rotary, 1 if interleaved else 0)
+        cp = cos_sin.data_ptr()
+    d = _append_desc.pack(code, batch, q_heads, stride, qp, kp, vp, op, q_layer, q_token, k_layer, k_token, v_layer, v_token,
+                          tables.data_ptr(), fp, np_, pp, cp, positions, rotary, 1 if interleaved else 0)
     _check(_lib.llmig_append_rotary(pool.handle, d, _stream(stream)), "llmig_append_rotary")
     _used_on(stream, q, k, v, q_out, tables, cos_sin)
 
@@ -637,9 +645,9 @@ def llmig_key_bounds(pool: Pool, bounds: Pool, tables: torch.Tensor, from_toks, 
     ctx_lens[b]) of each sequence were written.  bounds: a pool of block_size
     1 with the cache's layers, blocks, heads, head_dim and type, whose K
     tensors take the least and V tensors the largest key of each block."""
-    dtype = pool.k[0].dtype
+    dtype = pool.dtype
     code = _type_code(dtype, "the pool")
-    if bounds.k[0].dtype != dtype:
+    if bounds.dtype is not dtype:
         raise ValueError("bounds must be of the pool's type")
     fp, batch, f = _lens(from_toks)
     cp, count, c = _lens(ctx_lens)
@@ -674,7 +682,7 @@ def llmig_select_blocks(bounds: Pool, block_size: int, q: torch.Tensor, tables: 
     allow a score to reach.  q: CUDA [L][B][Hq][D]; blocks: CUDA int32
     [L][B][kv_heads][count], ascending block numbers, then -1."""
     code = _type_code(q.dtype, "q")
-    if not q.is_cuda or not q.is_contiguous() or q.dim() != 4 or q.dtype != bounds.k[0].dtype:
+    if not q.is_cuda or not q.is_contiguous() or q.dim() != 4 or q.dtype is not bounds.dtype:
         raise ValueError("q must be a contiguous CUDA [layers][batch][q_heads][head_dim] tensor of the bounds' type")
     layers, batch, q_heads, dim = q.shape
     if layers != bounds.num_layers or dim != bounds.head_dim:
@@ -696,7 +704,7 @@ def _decode_args(pool: Pool, q: torch.Tensor, tables: torch.Tensor, ctx_lens, ou
     """Checks what the decode attentions share; returns (type code, batch, query
     heads, table stride, address of the lengths, keepalive)."""
     code = _type_code(q.dtype, "q")
-    if not q.is_cuda or not q.is_contiguous() or q.dim() != 4 or q.dtype != pool.k[0].dtype:
+    if not q.is_cuda or not q.is_contiguous() or q.dim() != 4 or q.dtype is not pool.dtype:
         raise ValueError("q must be a contiguous CUDA [layers][batch][q_heads][head_dim] tensor of the pool's type")
     layers, batch, q_heads, dim = q.shape
     if layers != pool.num_layers or dim != pool.head_dim:
