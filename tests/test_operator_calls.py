@@ -123,7 +123,7 @@ def test_prefix_is_read_once_only_where_that_pays(call):
         dict(op="prefix", ctx_lens=[3000] * 30, prefix_blocks=0, **many)])
     once = ["prefix_rows", "attn_partial_mfma", "prefix_join"]
     assert kernels(short) == ["attn_partial_mfma"] and kernels(shared) == once and kernels(split) == once
-    assert shared["launches"][0]["template"][2] == 1 and split["launches"][0]["template"][2] == 4
+    assert shared["launches"][0]["template"][2] == 2 and split["launches"][0]["template"][2] == 4
     for x in (lone, none):
         assert kernels(x)[0] == "attn_partial_mfma" and "prefix_rows" not in kernels(x)
 
