@@ -377,6 +377,14 @@ __host__ __device__ inline uint32_t attn_blk_slots(uint32_t part_tokens, uint32_
 //               and their V rows count as zeros, whatever the pool holds there.
 //  kAttnOwn     the tokens of each sequence behind a prefix that prefix_rows
 //               (prefix_attention.h) computes: every item leaves a record.
+// Attention over listed blocks and behind a prefix takes fp16 weights times 2^7
+// (sums and products alike, so results keep their size): of small weights beside
+// a large one the low part then rounds 2^-32, not 2^-25, of the largest.
+constexpr float attn_weights_up(int bf16)
+{
+    return bf16 ? 0.f : 7.f;
+}
+
 enum AttnMode { kAttnPlain = 0, kAttnMigrating = 1, kAttnListed = 2, kAttnOwn = 3 };
 
 template <int MODE> struct AttnArgsOf { typedef AttnArgs type; };
@@ -762,10 +770,11 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
         // where a partition starts decides what "so far" holds.
         const float m_new = fmaxf(m, mx), m_sub = m_new == -INFINITY ? 0.f : m_new;
         const float c = exp2f(m - m_sub);
+        constexpr float up = LISTED || MODE == kAttnOwn ? attn_weights_up(BF16) : 0.f;
         float p[4], ps = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            p[i] = exp2f(sc[i] - m_sub);
+            p[i] = exp2f(up > 0.f ? sc[i] - (m_sub - up) : sc[i] - m_sub);
             ps += p[i];
         }
         ps += __shfl_xor(ps, 16);

@@ -243,8 +243,8 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
                     s[i] = first + 8u * (i / 4) + i % 4 < t_end ? s[i] : -INFINITY;
             }
             // The maximum that weights are taken against moves only when a score
-            // exceeds it by 2^8: the sums have the room, and the accumulators are
-            // rescaled seldom.
+            // exceeds it by 2^8: the sums have the room (fp16 weights reach 2^15), and
+            // the accumulators are rescaled seldom.
             float mx = s[0];
 #pragma unroll
             for (int i = 1; i < 16; ++i)
@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
                     acc[mt] = acc[mt] * c;
                 m = m_new;
             }
-            const float m_sub = m == -INFINITY ? 0.f : m;
+            const float m_sub = m == -INFINITY ? 0.f : m - attn_weights_up(BF16);
             // From here on to the end of the step products and weights alternate:
             // the next 32 tokens' scores beside the first 16 tokens' weights, those
             // tokens' part of O^T += V^T . P^T beside the other 16 tokens' weights.

@@ -222,7 +222,7 @@ class Pool:
         self.k, self.v, self.dtype = list(k_layers), list(v_layers), t0.dtype
         self.num_layers, self.num_blocks, self.block_size = len(k_layers), nb, bs
         self.num_kv_heads, self.head_dim, self.elem_bytes = heads, dim, t0.element_size()
-        self.layouts = (int(layouts[0]), int(layouts[1]))
+        self.layouts, self.device_index = (int(layouts[0]), int(layouts[1])), t0.device.index
         self.tile_bytes = _lib.llmig_pool_tile_bytes(handle)
         self.slot_bytes = self.tile_bytes // bs
 
@@ -559,9 +559,10 @@ def _type_code(dtype, what: str) -> int:
     return code
 
 
-def _device_tables(tables: torch.Tensor, batch: int) -> int:
-    """Checks block tables; returns their row stride."""
-    if tables.dtype != torch.int32 or not tables.is_cuda or not tables.is_contiguous() or tables.dim() != 2:
+def _device_tables(pool: Pool, tables: torch.Tensor, batch: int) -> int:
+    """Checks block tables; returns their row stride.  (Here as below, a tensor
+    on the CPU or on another GPU than the pool's is refused.)"""
+    if tables.dtype != torch.int32 or tables.get_device() != pool.device_index or not tables.is_contiguous() or tables.dim() != 2:
         raise ValueError("tables must be a contiguous CUDA int32 [batch][stride] tensor")
     rows, stride = tables.shape
     if rows < batch:
@@ -569,17 +570,17 @@ def _device_tables(tables: torch.Tensor, batch: int) -> int:
     return stride
 
 
-def _workspace(workspace: torch.Tensor) -> int:
-    if not workspace.is_cuda or not workspace.is_contiguous():
+def _workspace(pool: Pool, workspace: torch.Tensor) -> int:
+    if workspace.get_device() != pool.device_index or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous CUDA tensor")
     return workspace.nbytes
 
 
-def _token_rows(t: torch.Tensor, dtype, shape, name: str):
+def _token_rows(pool: Pool, t: torch.Tensor, shape, name: str):
     """Checks rows of new tokens, [L][tokens][heads][D]; returns their address,
     layer and token strides (0 along an axis of one entry, whose stride may be
     any)."""
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
+    if t.shape != shape or t.dtype is not pool.dtype or t.get_device() != pool.device_index:
         raise ValueError(f"{name} must be a CUDA [layers][tokens][heads][head_dim] tensor of the pool's type")
     layers, tokens, heads, dim = shape
     layer, token, head, one = t.stride()
@@ -614,23 +615,24 @@ def llmig_append_rotary(pool: Pool, k: torch.Tensor, v: torch.Tensor, tables: to
     total = sum(n) if type(n) is array else int(n.sum(dtype=np.int64))
     layers, dim = pool.num_layers, pool.head_dim
     shape = (layers, total, pool.num_kv_heads, dim)
-    kp, k_layer, k_token = _token_rows(k, dtype, shape, "k")
-    vp, v_layer, v_token = _token_rows(v, dtype, shape, "v")
+    kp, k_layer, k_token = _token_rows(pool, k, shape, "k")
+    vp, v_layer, v_token = _token_rows(pool, v, shape, "v")
     qp = op = q_heads = q_layer = q_token = 0
     if q is not None:
         if q.dim() != 4 or q_out is None:
             raise ValueError("q must be a [layers][tokens][heads][head_dim] tensor and come with q_out")
         q_heads = q.shape[2]
-        qp, q_layer, q_token = _token_rows(q, dtype, (layers, total, q_heads, dim), "q")
-        if q_out.shape != q.shape or q_out.dtype is not dtype or not q_out.is_cuda or not q_out.is_contiguous():
+        qp, q_layer, q_token = _token_rows(pool, q, (layers, total, q_heads, dim), "q")
+        if q_out.shape != q.shape or q_out.dtype is not dtype or q_out.get_device() != pool.device_index or not q_out.is_contiguous():
             raise ValueError("q_out must be a contiguous CUDA tensor of q's shape and type")
         op = q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q and q_out come together")
-    stride = _device_tables(tables, batch)
+    stride = _device_tables(pool, tables, batch)
     cp = positions = rotary = 0
     if cos_sin is not None:
-        if cos_sin.dtype is not torch.float32 or not cos_sin.is_cuda or not cos_sin.is_contiguous() or cos_sin.dim() != 2:
+        if cos_sin.dtype is not torch.float32 or cos_sin.get_device() != pool.device_index or not cos_sin.is_contiguous() or \
+                cos_sin.dim() != 2:
             raise ValueError("cos_sin must be a contiguous CUDA float32 [positions][rotary_dim] tensor")
         positions, rotary = cos_sin.shape
         cp = cos_sin.data_ptr()
@@ -653,7 +655,7 @@ def llmig_key_bounds(pool: Pool, bounds: Pool, tables: torch.Tensor, from_toks, 
     cp, count, c = _lens(ctx_lens)
     if count != batch:
         raise ValueError("from_toks and ctx_lens must hold one number per sequence")
-    stride = _device_tables(tables, batch)
+    stride = _device_tables(pool, tables, batch)
     _check(_lib.llmig_key_bounds(pool.handle, bounds.handle, code, batch, tables.data_ptr(), stride, fp, cp,
                                  _stream(stream)), "llmig_key_bounds")
     _used_on(stream, tables)
@@ -667,10 +669,10 @@ def select_workspace_bytes(bounds: Pool, block_size: int, ctx_lens) -> int:
     return n.value
 
 
-def _block_lists(blocks: torch.Tensor, layers: int, batch: int, heads: int) -> int:
+def _block_lists(pool: Pool, blocks: torch.Tensor, batch: int) -> int:
     """Checks lists of blocks; returns their length."""
-    if blocks.dtype != torch.int32 or not blocks.is_cuda or not blocks.is_contiguous() or blocks.dim() != 4 or \
-            blocks.shape[:3] != (layers, batch, heads):
+    if blocks.dtype != torch.int32 or blocks.get_device() != pool.device_index or not blocks.is_contiguous() or \
+            blocks.dim() != 4 or blocks.shape[:3] != (pool.num_layers, batch, pool.num_kv_heads):
         raise ValueError("blocks must be a contiguous CUDA int32 [layers][batch][kv_heads][count] tensor")
     return blocks.shape[3]
 
@@ -682,7 +684,7 @@ def llmig_select_blocks(bounds: Pool, block_size: int, q: torch.Tensor, tables: 
     allow a score to reach.  q: CUDA [L][B][Hq][D]; blocks: CUDA int32
     [L][B][kv_heads][count], ascending block numbers, then -1."""
     code = _type_code(q.dtype, "q")
-    if not q.is_cuda or not q.is_contiguous() or q.dim() != 4 or q.dtype is not bounds.dtype:
+    if q.get_device() != bounds.device_index or not q.is_contiguous() or q.dim() != 4 or q.dtype is not bounds.dtype:
         raise ValueError("q must be a contiguous CUDA [layers][batch][q_heads][head_dim] tensor of the bounds' type")
     layers, batch, q_heads, dim = q.shape
     if layers != bounds.num_layers or dim != bounds.head_dim:
@@ -690,9 +692,9 @@ def llmig_select_blocks(bounds: Pool, block_size: int, q: torch.Tensor, tables: 
     cp, count, c = _lens(ctx_lens)
     if count != batch:
         raise ValueError("ctx_lens must hold one length per sequence of q")
-    stride = _device_tables(tables, batch)
-    listed = _block_lists(blocks, layers, batch, bounds.num_kv_heads)
-    nbytes = _workspace(workspace)
+    stride = _device_tables(bounds, tables, batch)
+    listed = _block_lists(bounds, blocks, batch)
+    nbytes = _workspace(bounds, workspace)
     _check(_lib.llmig_select_blocks(bounds.handle, code, int(block_size), q.data_ptr(), batch, q_heads,
                                     tables.data_ptr(), stride, cp, int(keep_first), int(keep_last), listed,
                                     workspace.data_ptr(), nbytes, blocks.data_ptr(), _stream(stream)),
@@ -704,17 +706,17 @@ def _decode_args(pool: Pool, q: torch.Tensor, tables: torch.Tensor, ctx_lens, ou
     """Checks what the decode attentions share; returns (type code, batch, query
     heads, table stride, address of the lengths, keepalive)."""
     code = _type_code(q.dtype, "q")
-    if not q.is_cuda or not q.is_contiguous() or q.dim() != 4 or q.dtype is not pool.dtype:
+    if q.get_device() != pool.device_index or not q.is_contiguous() or q.dim() != 4 or q.dtype is not pool.dtype:
         raise ValueError("q must be a contiguous CUDA [layers][batch][q_heads][head_dim] tensor of the pool's type")
     layers, batch, q_heads, dim = q.shape
     if layers != pool.num_layers or dim != pool.head_dim:
         raise ValueError("q must be [layers][batch][q_heads][head_dim] of the pool's layers and head_dim")
-    if out.dtype != torch.float32 or not out.is_cuda or not out.is_contiguous() or out.shape != q.shape:
+    if out.dtype != torch.float32 or out.get_device() != pool.device_index or not out.is_contiguous() or out.shape != q.shape:
         raise ValueError("out must be a contiguous CUDA float32 tensor shaped like q")
     cp, count, c = _lens(ctx_lens)
     if count != batch:
         raise ValueError("ctx_lens must hold one length per sequence of q")
-    return code, batch, q_heads, _device_tables(tables, batch), cp, c
+    return code, batch, q_heads, _device_tables(pool, tables, batch), cp, c
 
 
 def decode_blocks_workspace_bytes(pool: Pool, ctx_lens, q_heads: int, count: int) -> int:
@@ -730,8 +732,8 @@ def llmig_decode_attention_blocks(pool: Pool, q: torch.Tensor, tables: torch.Ten
     """llmig_decode_attention of each (layer, sequence, KV head) over the
     blocks that blocks (CUDA int32 [L][B][kv_heads][count]) lists for it."""
     code, batch, q_heads, stride, cp, c = _decode_args(pool, q, tables, ctx_lens, out)
-    listed = _block_lists(blocks, pool.num_layers, batch, pool.num_kv_heads)
-    nbytes = _workspace(workspace)
+    listed = _block_lists(pool, blocks, batch)
+    nbytes = _workspace(pool, workspace)
     _check(_lib.llmig_decode_attention_blocks(pool.handle, code, q.data_ptr(), batch, q_heads, tables.data_ptr(), stride,
                                               cp, blocks.data_ptr(), listed, scale, workspace.data_ptr(), nbytes,
                                               out.data_ptr(), _stream(stream)), "llmig_decode_attention_blocks")
@@ -751,7 +753,7 @@ def llmig_decode_attention_prefix(pool: Pool, q: torch.Tensor, tables: torch.Ten
     """llmig_decode_attention of a batch whose table rows begin with the same
     prefix_blocks blocks: those are read once for all sequences."""
     code, batch, q_heads, stride, cp, c = _decode_args(pool, q, tables, ctx_lens, out)
-    nbytes = _workspace(workspace)
+    nbytes = _workspace(pool, workspace)
     _check(_lib.llmig_decode_attention_prefix(pool.handle, code, q.data_ptr(), batch, q_heads, tables.data_ptr(), stride,
                                               cp, int(prefix_blocks), scale, workspace.data_ptr(), nbytes,
                                               out.data_ptr(), _stream(stream)), "llmig_decode_attention_prefix")

@@ -59,6 +59,24 @@ def attention(k, v, q, scale, dtype):
     return out, tol
 
 
+def small_weights(kv, q, tables, b, n):
+    """Gives sequence b's first token a score of 0 and values of 0, its other n -
+    1 ones weights of 2^-15.3 and values of 1: fp16 holds such a weight in steps
+    of 2^-24 of the largest, times 2^7 in steps of 2^-31, half of one off at most.
+    The bound of (1 - weight of the first): every weight off by 2^-32, and the
+    relative part of attention()."""
+    bs = kv.shape[3]
+    q[:, b] = 0
+    q[:, b, :, 0] = 1
+    blk, slot = rows_of(tables, b, range(n), bs)
+    kv[0][:, blk, slot], kv[1][:, blk, slot] = 0, 1
+    kv[0][:, blk[1:], slot[1:], :, 0] = -10.6
+    kv[1][:, blk[0], slot[0]] = 0
+    w = (n - 1) * math.exp(float(torch.tensor(-10.6, dtype=kv.dtype)))
+    rel = EPS_P["fp16"] + LAMBDA * U32 * (2 * math.sqrt(64 + -(-n // 16)) + 4 * (math.sqrt(kv.shape[5]) + 2) * 10.7 + 2)
+    return w / (1 + w), n * 2.0 ** -32 + w / (1 + w) * rel + U32
+
+
 def decode(kv, q, tables, scale, dtype, tokens_of):
     """kv [2][L][blocks][bs][H][D], q [L][B][Hq][D] on the CPU; tokens_of(l, b, g)
     lists the tokens a row attends to."""

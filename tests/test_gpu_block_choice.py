@@ -228,6 +228,15 @@ def test_a_block_listed_twice_counts_twice():
     attend(kv, q, tables, [100], torch.tensor([3, 0, 3, 6, 6], dtype=torch.int32).view(1, 1, 1, 5), "bf16")
 
 
+@pytest.mark.parametrize("D,bs,n", [(128, 16, 700), (64, 12, 2100)])
+def test_small_weights_beside_a_large_one(D, bs, n):
+    kv, q, tables, _ = make(1, 2, 4, D, bs, "fp16", [n])
+    want, tol = oc.small_weights(kv, q, tables, 0, n)
+    lists = torch.arange(-(-n // bs), dtype=torch.int32).expand(1, 1, 2, -1).contiguous()
+    out = attend(kv, q, tables, [n], lists, "fp16", scale=1.0)
+    assert float((out.double() - want).abs().max()) <= tol
+
+
 @pytest.mark.parametrize("bs", [16, 8, 12, 2])
 def test_lists_that_name_nothing(bs):
     kv, q, tables, _ = make(1, 2, 2, 64, bs, "bf16", [100, 5])

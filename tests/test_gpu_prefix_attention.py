@@ -87,7 +87,7 @@ def test_matches_attention(case):
     run(*setup(L, H, G, D, bs, dtype, ctx, prefix), ctx, prefix, dtype)
 
 
-# Up to 32, up to 64 and more rows a KV head; one workgroup a partition and two;
+# Up to 64 and more rows a KV head; one workgroup a partition and two;
 # blocks of 16 tokens or a multiple, and others; prefixes that end inside a tile.
 SHARED = [
     (1, 16, 1, 128, 16, "bf16", [688 + i for i in range(30)], 43),
@@ -147,6 +147,16 @@ def test_rising_scores(dtype, step):
         blk, slot = oc.rows_of(tables, b, range(CTX[b]), 16)
         kv[0, 0, blk, slot, :, 0] = (torch.arange(CTX[b]) * step / 8).to(kv.dtype)[:, None]
     run(kv, q, tables, CTX, PREFIX, dtype, scale=1.0, once=True)
+
+
+@pytest.mark.parametrize("own", [0, 60])
+def test_small_weights_beside_a_large_one(own):
+    ctx = [688 + own] * 30
+    kv, q, tables = setup(*SHAPE, "fp16", ctx, PREFIX)
+    for b in range(30):
+        want, tol = oc.small_weights(kv, q, tables, b, 688 + own)
+    out = run(kv, q, tables, ctx, PREFIX, "fp16", scale=1.0, once=True)
+    assert float((out.double() - want).abs().max()) <= tol
 
 
 @pytest.mark.parametrize("where", ["prefix", "own"])
