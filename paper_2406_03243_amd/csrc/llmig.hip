@@ -1906,8 +1906,8 @@ int llmig_decode_attention_prefix(const llmig_pool *pool, int32_t dtype, const v
     a.by_block = divisor(a.block_size);
     std::memcpy(a.member, p.member, sizeof(a.member));
     void *args[] = {&a};
-    hipError_t e = hipLaunchKernel(prefix_kernel_for(dtype, pool->head_dim, p.cut.wm, pool->block_size % 16 == 0), dim3(static_cast<uint32_t>(grid)),
-                                   dim3(kThreads), args, 0, st);
+    hipError_t e = hipLaunchKernel(prefix_kernel_for(dtype, pool->head_dim, p.cut.wm, pool->block_size % 8 == 0),
+                                   dim3(static_cast<uint32_t>(grid)), dim3(kThreads), args, 0, st);
     if (e != hipSuccess)
         return hip_error(e);
     AttnOwnArgs o;

@@ -92,8 +92,8 @@ __device__ __forceinline__ void split_weights(float p0, float p1, uint32_t *hi, 
     }
 }
 
-// The rows of 16 tokens of a block: a multiple of 16 tokens a block (ALIGNED)
-// puts each such group in one, so its row is found with scalar instructions.
+// A multiple of 8 tokens a block (ALIGNED) puts each 8 tokens in one, so their
+// row is found with scalar instructions.
 //
 // One workgroup: a partition of one (layer, KV head) against 32 * WM query
 // rows.  Of its four wavefronts WM split the rows, 32 each (the columns of one
@@ -164,25 +164,28 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
     static_assert(RPI % 16 == 0, "a thread's rows swizzle alike");
     const uint32_t th = threadIdx.x / LPR, tc = threadIdx.x % LPR;
     uint32_t ids[CPT];
-    // ALIGNED: the first of the 16 tokens (t_end is a multiple of 16) to which the
+    // ALIGNED: the first of the 8 tokens (t_end is a multiple of 8) to which the
     // wavefront's rows of load i belong; else the thread's token.
     const uint32_t wave_row = wave * (64u / LPR);
     auto token_of = [&](uint32_t t0, uint32_t i) {
-        return ALIGNED ? min(t0 + (i * RPI + wave_row) / 16u * 16u, t_end - 16u) : min(t0 + i * RPI + th, t_end - 1u);
+        return ALIGNED ? min(t0 + (i * RPI + wave_row) / 8u * 8u, t_end - 8u) : min(t0 + i * RPI + th, t_end - 1u);
     };
-    const uint64_t lane_row = ALIGNED ? static_cast<uint64_t>(th % 16u) * a.kv_heads * RB : 0u;
+    auto block_of = [&](uint32_t t) {       // (ALIGNED: the divisor is not 1)
+        return ALIGNED ? __umulhi(t, a.by_block.m) >> a.by_block.shift : divide(t, a.by_block);
+    };
+    const uint64_t lane_row = ALIGNED ? static_cast<uint64_t>(th % 8u) * a.kv_heads * RB : 0u;
     const uint8_t *k_lane = kbase + lane_row + 16u * (tc ^ k_swizzle(th)), *v_lane = vbase + lane_row + 16u * (tc ^ v_swizzle(th));
     auto look_up = [&](uint32_t t0) {
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
-            const uint32_t blk = divide(token_of(t0, i), a.by_block);
+            const uint32_t blk = block_of(token_of(t0, i));
             ids[i] = ALIGNED ? static_cast<uint32_t>(id_entry(a.table, uniform(blk))) : static_cast<uint32_t>(a.table[blk]);
         }
     };
     auto fetch = [&](uint8_t *tile, uint32_t t0) {
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
-            const uint32_t t = token_of(t0, i), blk = divide(t, a.by_block);
+            const uint32_t t = token_of(t0, i), blk = block_of(t);
             const uint64_t slot = static_cast<uint64_t>(min(ids[i], a.num_blocks - 1u)) * a.block_size + (t - blk * a.block_size);
             const uint64_t at = (slot * a.kv_heads + g) * RB;
             uint8_t *to = tile + (i * RPI + wave_row) * RB;
