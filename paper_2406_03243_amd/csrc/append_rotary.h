@@ -278,7 +278,12 @@ __device__ __forceinline__ void move_pair(const AppendArgs &a, uint32_t kind, ui
     }
 }
 
-// Unit: (token, LG layers).  A token's rows, one after the other.
+// Unit: (token, LG layers).  A token's rows, one after the other: each row is read
+// and written once as whole lines, and nothing is shared but the table's entries.
+// Bound by HBM where there is enough of it: queries of 32 heads of 128, 8 layers of
+// 5777 tokens, 757 MB in 130 us, 5.8 TB/s; a decode step's tokens (32 layers of 61
+// tokens, 32 query and 8 KV heads) are one round of workgroups, 48 MB in 13.2 us,
+// where a plain copy of 48 MB takes 10.5; one token of one layer is a launch, 3.5 us.
 template <int BF16, int LG, int FAST>
 __global__ void __launch_bounds__(kThreads) append_rotary_rows(const AppendArgs a)
 {
@@ -329,7 +334,9 @@ __device__ __forceinline__ BlockSlots block_slots(const AppendArgs &a, uint32_t 
 // answers with a third of its rate, so a workgroup takes the tokens of a block.
 //
 // HCNX.  Unit: (block, LG layers); a lane takes a pair of chunks of one slot, a
-// wavefront 8 slots of 8 pairs: it reads and writes whole 128-byte lines.
+// wavefront 8 slots of 8 pairs: it reads and writes whole 128-byte lines.  Keys of
+// 32 heads of 128, 8 layers of 5777 tokens, 757 MB in 146 us, 5.2 TB/s (the writes
+// go to one of eight places of a tile each).
 template <int BF16, int LG, int FAST>
 __global__ void __launch_bounds__(kThreads) append_rotary_slots(const AppendArgs a)
 {
@@ -350,6 +357,8 @@ __global__ void __launch_bounds__(kThreads) append_rotary_slots(const AppendArgs
 // HDN.  Unit: (block, layer); a lane turns 8 dims of 8 slots round in
 // registers, and LDS puts the lanes' pieces in the tile's order, so that a
 // wavefront stores whole KiB.  Slots that the call does not write keep theirs.
+// Values of the call above, 757 MB in 152 us, 5.0 TB/s; LDS holds four workgroups a
+// CU, and bank conflicts take 5% of the cycles.
 template <int BF16>
 __global__ void __launch_bounds__(kThreads) append_rotary_dims(const AppendArgs a)
 {

@@ -47,7 +47,9 @@ __device__ __forceinline__ float larger_of(float a, float b)
 
 // A lane takes 8 dims of one block's keys over its row's share of the tokens,
 // eight loads in flight; the rows meet in LDS.  A NaN key makes both of its
-// bounds NaN.
+// bounds NaN.  Every key is read once, so HBM bounds it: prompts of up to 32768
+// tokens, 4 layers of 8 heads of 128, 515 MB in 90 us, 5.7 TB/s; one block each of
+// 32 requests, 32 layers, 22 MB in 7.9 us, of which some 4 start and end a launch.
 template <int BF16>
 __global__ void __launch_bounds__(kThreads) key_bounds_rows(const BoundsArgs a)
 {
@@ -177,8 +179,10 @@ __device__ __forceinline__ double sums_of_four(const double *s, uint32_t c)
 // A lane takes 8 dims of one KV head, its sums P and N in registers, over the
 // consecutive blocks of its row of lanes, four blocks' bounds in flight; the D / 8
 // lanes of a head add up, and each keeps the score of one block in D / 8, so that
-// scores leave as whole lines.
-
+// scores leave as whole lines.  The bounds are read once: 12 requests of up to 65536
+// tokens, 4 layers of 8 heads of 128, 352 MB in 68 us, 5.2 TB/s, with the 64-bit
+// sums taking half of the vector unit's time (sums across lanes through LDS, and
+// without the bounds' loads a step ahead, 79 us).
 template <int BF16, int D>
 __global__ void __launch_bounds__(kThreads) score_blocks(const SelectArgs a)
 {
@@ -350,7 +354,9 @@ __device__ __forceinline__ void exclusive_sums(uint32_t *x)
 // workgroup a row: a radix search for the key of the last one listed, a byte a
 // pass, which ends as soon as all keys that begin alike are listed; then the
 // listed ones leave in order.  KPT: a thread holds that many keys, which are
-// read once; 0: rows too long for that read them from memory in each pass.
+// read once; 0: rows too long for that read them from memory in each pass.  A pass
+// is a chain of LDS adds and three barriers, some 0.5 us, and that chain is what a
+// call takes: 24 rows of up to 563 blocks 5.6 us, 384 of up to 4096 12.
 template <int T, int KPT>
 __global__ void __launch_bounds__(T) list_blocks(const SelectArgs a)
 {
