@@ -415,9 +415,18 @@ __global__ void __launch_bounds__(kThreads) append_rotary_dims(const AppendArgs 
     }
 }
 
-// From this many new tokens of a sequence on, tiles whose tokens do not lie in
-// one piece are written block by block.
-constexpr int64_t kAppendBlockTokens = 2;
+// Whether tiles whose tokens do not lie in one piece are written block by block: one
+// or two launches more, and a workgroup for a block that may get a single token, so
+// it takes enough tokens a block, and bytes (of keys and values).  Token by token /
+// block by block, HCNX keys and HDN values of 16 tokens a block, us: 0.3 MB 8.8 /
+// 14.9, 5.0 MB (10 tokens a block) 20.8 / 23.3, 5.3 MB (full ones) 21.2 / 22.2, 9.7 MB
+// 35.2 / 26.7, 21 MB 74.7 / 42.0, 30 MB (5 tokens a block) 110 / 92, 8.5 MB of one or two
+// 37.7 / 57.4; both HCNX 12.7 / 19.0 at 5.3 MB, 28.1 / 23.5 at 9.7; both HDN 32.0 / 29.3
+// and 54.9 / 33.8.
+inline bool append_by_blocks(int64_t tokens, int64_t blocks, int64_t bytes)
+{
+    return tokens >= 4 * blocks && bytes >= 6 << 20;
+}
 
 // Layers of a token that a workgroup moves, for `work` workgroups of one layer.
 // With two the setup (the sequence, the block, the table's entries) is paid half

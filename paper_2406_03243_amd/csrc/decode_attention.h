@@ -369,6 +369,9 @@ __host__ __device__ inline uint32_t attn_blk_slots(uint32_t part_tokens, uint32_
 // that never change).  A partition has at most 64 units per wavefront.  Other
 // block sizes stage the block ids in LDS and look each token's up.
 //
+// UNITS 2 (kAttnListed and kAttnOwn): the workgroup's four wavefronts take four KV
+// heads of an item, each by itself, all of its tokens (attn_lone_heads).
+//
 // Attention over listed blocks and behind a prefix takes fp16 weights times 2^7
 // (sums and products alike, so results keep their size): of small weights beside
 // a large one the low part then rounds 2^-32, not 2^-25, of the largest.
@@ -400,7 +403,7 @@ template <int BF16, int D, int MODE, int UNITS>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(MODE == kAttnMigrating ? 3 : 4, 8)))
 attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
 {
-    constexpr bool MIG = MODE == kAttnMigrating, LISTED = MODE == kAttnListed;
+    constexpr bool MIG = MODE == kAttnMigrating, LISTED = MODE == kAttnListed, LONE = UNITS == 2;
     constexpr int KS = D / 32;            // k-steps of the QK product
     constexpr int MT = D / 16;            // 16-dim tiles of the PV product
     constexpr int LPR = D / 8;            // lanes per row in the K and V loads (16 bytes each)
@@ -432,7 +435,7 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
     // attn_layer_by_layer for the calls that don't).
     uint32_t item, g, layer;
     {
-        const uint32_t H = a.kv_heads, lin = blockIdx.x;
+        const uint32_t H = LONE ? (a.kv_heads + 3u) / 4u : a.kv_heads, lin = blockIdx.x;
         const uint32_t full = gridDim.x - gridDim.x % (8u * H);
         uint32_t unit;                    // (item, layer) in the launch's order
         if (lin < full) {
@@ -475,6 +478,10 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
     const uint32_t G = a.q_heads / a.kv_heads;
     const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
     const uint32_t wv = uniform(wave);
+    const bool idle = LONE && 4u * g + wv >= a.kv_heads;
+    if constexpr (LONE)
+        g = min(4u * g + wv, a.kv_heads - 1u);
+    constexpr int32_t kStride = LONE ? 16 : 64;     // tokens between a wavefront's groups
     const uint32_t r16 = lane % 16, g4 = lane / 16;
     const int32_t bs = static_cast<int32_t>(a.block_size);
 
@@ -505,7 +512,7 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
         }
         return held;
     };
-    const int32_t tg0 = start + 16 * static_cast<int32_t>(wv);
+    const int32_t tg0 = idle ? end : LONE ? start : start + 16 * static_cast<int32_t>(wv);
     const int32_t first_blk = UNITS ? 0 : start / bs;
     int32_t *sh_dst = sh_blk + attn_blk_slots(a.part_tokens, a.block_size);
     // UNITS: lane l's unit is tokens tg0 + 64 * (l / 2) + 8 * (l % 2) .. + 7:
@@ -517,7 +524,7 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
     int32_t unit_held = 0;     // LISTED: rows of the unit that hold tokens
     if constexpr (UNITS) {
         if (tg0 < end) {
-            const int32_t t = min(tg0 + 64 * static_cast<int32_t>(lane / 2) + 8 * static_cast<int32_t>(lane % 2), end - 1);
+            const int32_t t = min(tg0 + kStride * static_cast<int32_t>(lane / 2) + 8 * static_cast<int32_t>(lane % 2), end - 1);
             const int32_t blk = t / bs;
             if constexpr (LISTED) {
                 uint32_t block;
@@ -592,7 +599,7 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
     };
     auto request_group = [&](int32_t t0) {
         if constexpr (UNITS) {
-            const uint32_t u0 = static_cast<uint32_t>(t0 - tg0) / 32u;      // the group's first unit (lane)
+            const uint32_t u0 = static_cast<uint32_t>(t0 - tg0) / (kStride / 2u);      // the group's first unit (lane)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const uint32_t slot = __builtin_amdgcn_readlane(unit_slot, u0 + half);
@@ -703,7 +710,7 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
     for (int ks = 0; ks < KS; ++ks)
         asm volatile("" : "+v"(qf[ks]));
     bool stored = false;    // the group before this one issued 2 * KS stores, after this one's request
-    for (int32_t tg = tg0; tg < end; tg += 64) {
+    for (int32_t tg = tg0; tg < end; tg += kStride) {
         // this group's rows have landed; loads and stores complete in order,
         // so the stores behind them need not have
         if (MIG && stored)
@@ -718,7 +725,7 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
         uint32_t held = 15u;
         if constexpr (LISTED) {
             if constexpr (UNITS) {
-                const uint32_t u0 = static_cast<uint32_t>(tg - tg0) / 32u;
+                const uint32_t u0 = static_cast<uint32_t>(tg - tg0) / (kStride / 2u);
                 const int32_t h0 = static_cast<int32_t>(__builtin_amdgcn_readlane(unit_held, u0)),
                               h1 = static_cast<int32_t>(__builtin_amdgcn_readlane(unit_held, u0 + 1));
                 const int32_t left = (g4 < 2 ? h0 : h1) - 4 * static_cast<int32_t>(g4 % 2);
@@ -744,8 +751,8 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
         if (carry)
             read_rows();
         // (the reads have returned: the next group's rows may overwrite them)
-        if (tg + 64 < end)
-            request_group(tg + 64);
+        if (tg + kStride < end)
+            request_group(tg + kStride);
         if (MIG) {
             // the stores stay behind the request: the wait above counts on it
             asm volatile("" ::: "memory");
@@ -831,16 +838,19 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
     auto put = [&](uint32_t at, f32x4_t v) {
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), ro, at * 4, 0, kResultStore);
     };
-    for (uint32_t x = threadIdx.x; x < G * (D / 4); x += kThreads) {
+    // LONE: every wavefront its own rows, of its head
+    const uint32_t w_first = LONE ? wv : 0u;
+    constexpr uint32_t kMerged = LONE ? 1 : 4;
+    for (uint32_t x = LONE ? lane : threadIdx.x; x < (idle ? 0u : G * (D / 4)); x += LONE ? 64 : kThreads) {
         const uint32_t row = x / (D / 4), d4 = x % (D / 4);
         float mm = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-            mm = fmaxf(mm, sh_m[w][row]);
+        for (uint32_t w = 0; w < kMerged; ++w)
+            mm = fmaxf(mm, sh_m[w_first + w][row]);
         float ll = 0.f;
         f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (uint32_t w = w_first; w < w_first + kMerged; ++w) {
             const float c = mm == -INFINITY ? 0.f : exp2f(sh_m[w][row] - mm);
             ll += sh_l[w][row] * c;
             o += *reinterpret_cast<const f32x4_t *>(so + (w * 16 + row) * kMergeRow + 4 * d4) * c;
@@ -854,15 +864,19 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
     }
 }
 
+// units: 0, 1 or 2 (see attn_lone_heads)
 template <int BF16, int D, int MODE>
-const void *attn_kernel(bool units)
+const void *attn_kernel(int units)
 {
+    if constexpr (MODE == kAttnListed || MODE == kAttnOwn)
+        if (units == 2)
+            return reinterpret_cast<const void *>(&attn_partial_mfma<BF16, D, MODE, 2>);
     return units ? reinterpret_cast<const void *>(&attn_partial_mfma<BF16, D, MODE, 1>)
                  : reinterpret_cast<const void *>(&attn_partial_mfma<BF16, D, MODE, 0>);
 }
 
 template <int BF16, int D>
-const void *attn_kernel(AttnMode mode, bool units)
+const void *attn_kernel(AttnMode mode, int units)
 {
     switch (mode) {
     case kAttnMigrating:
@@ -876,7 +890,7 @@ const void *attn_kernel(AttnMode mode, bool units)
     }
 }
 
-const void *attn_kernel_for(int bf16, int head_dim, int group, AttnMode mode, bool units)
+const void *attn_kernel_for(int bf16, int head_dim, int group, AttnMode mode, int units)
 {
     if (group < 1 || group > 16 || (group & (group - 1)) != 0)
         return nullptr;
@@ -1005,6 +1019,21 @@ inline int attn_workgroups_per_cu(int64_t head_dim, int64_t workgroups, int64_t 
     if (!migrating && 5 * workgroups < 7 * full * kAttnCUs)
         return 0;
     return mean_tokens >= (head_dim == 64 ? 800 : 1500) ? full : 0;
+}
+
+// Whether each wavefront of a call over listed blocks, or over the tokens behind a
+// prefix, takes a KV head by itself (UNITS 2).  A workgroup costs some 5 ns of a call
+// however little it does, so many short sequences gain by a quarter of them; a
+// wavefront that walks a sequence alone takes 0.9 us per 16 tokens, which has to pass
+// while the others work.  `workgroups` of four wavefronts a head / a head each, up to
+// 16, 100, 200, 500 tokens, us: 320 of them 6.3 / 9.6, 8.5 / 11.7, ..; 1280 10.4 /
+// 8.4, 13.7 / 13.4, 18.2 / 19.9, 33.2 / 40.5; 2560 14.7 / 8.7, 21.7 / 16.4, 31.1 /
+// 27.9, 57.5 / 62.7; 8192 39.8 / 16.0, 59.7 / 42.3, 79.8 / 66.7, 159.1 / 158.7; 7680 of
+// head_dim 64 23.6 / 12.8, 31.9 / 23.8, 41.5 / 34.4, 80.1 / 72.7.  One KV head leaves
+// three wavefronts idle (1280 of them 10.7 / 12.1), two still gain (2560 15.7 / 12.8).
+inline bool attn_lone_heads(int64_t workgroups, int32_t longest, int64_t kv_heads)
+{
+    return kv_heads >= 2 && workgroups >= 1024 && longest <= std::min<int64_t>(512, workgroups / 12);
 }
 
 // Whether a call runs layer by layer instead of longest item first: batches of

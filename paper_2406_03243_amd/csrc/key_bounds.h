@@ -24,10 +24,11 @@ struct BoundsArgs {
     uint32_t num_layers, num_blocks, block_size, table_stride, tile_bytes, batch;
     uint32_t slot_chunks;        // 16-byte chunks of a token's keys, and of a block's bounds
     uint32_t rows;               // rows of lanes that share a block's tokens
+    uint32_t side;               // blocks side by side in a workgroup
     uint32_t one_each;           // every sequence has one block
     uint32_t first_item;
-    Divisor by_slice, by_block;  // by_block: division by the blocks of the call
-    Divisor by_chunk;            // by the chunks of a slice
+    Divisor by_slice, by_group;  // by_group: division by the groups of `side` blocks of the call
+    Divisor by_chunk, by_row;    // by the chunks of a slice, by rows
     uint32_t blocks;             // blocks of the call
     uint32_t block_end[kAppendMaxBatch];  // blocks of the first s + 1 sequences
     int32_t first_block[kAppendMaxBatch]; // first block of sequence s to bring up to date
@@ -46,28 +47,32 @@ __device__ __forceinline__ float larger_of(float a, float b)
 }
 
 // A lane takes 8 dims of one block's keys over its row's share of the tokens,
-// eight loads in flight; the rows meet in LDS.  A NaN key makes both of its
-// bounds NaN.  Every key is read once, so HBM bounds it: prompts of up to 32768
-// tokens, 4 layers of 8 heads of 128, 515 MB in 90 us, 5.7 TB/s; one block each of
-// 32 requests, 32 layers, 22 MB in 7.9 us, of which some 4 start and end a launch.
-template <int BF16>
+// eight loads in flight; the rows meet in LDS.  Blocks of few heads stand side by
+// side (SIDE), so that every lane has 8 tokens where the block has them (23 layers of
+// 2 heads of 64, 7 requests of up to 3431 tokens, 32 a block: a block a workgroup 58
+// us, 4 of them 20).  A NaN key makes both of its bounds NaN.  Every key is read once, so HBM bounds it: prompts of
+// up to 32768 tokens, 4 layers of 8 heads of 128, 515 MB in 90 us, 5.7 TB/s; one block
+// each of 32 requests, 32 layers, 22 MB in 7.9 us, of which some 4 start and end a
+// launch.
+template <int BF16, int SIDE>
 __global__ void __launch_bounds__(kThreads) key_bounds_rows(const BoundsArgs a)
 {
     __shared__ u32x4 part[2][kThreads];
     const uint32_t item = a.first_item + blockIdx.x;
     const uint32_t unit = divide(item, a.by_slice), slice = item - unit * a.by_slice.d;
-    const uint32_t layer = divide(unit, a.by_block), i = unit - layer * a.blocks;
+    const uint32_t layer = divide(unit, a.by_group), group = unit - layer * a.by_group.d;
+    const uint32_t set = divide(threadIdx.x, a.by_chunk), mine = threadIdx.x - set * a.by_chunk.d;
+    const uint32_t beside = SIDE ? divide(set, a.by_row) : 0u, r = set - beside * a.rows;
+    const uint32_t i = SIDE ? min(group * a.side + beside, a.blocks - 1u) : group;
     const uint32_t s = a.one_each ? i : sequence_of(a.block_end, a.batch, i);
     const uint32_t blk = static_cast<uint32_t>(a.first_block[s]) + i - (s > 0 ? a.block_end[s - 1] : 0u);
     const uint32_t id = table_id(a.tables, s, a.table_stride, blk);
     const uint32_t held = min(static_cast<uint32_t>(a.tokens[s]) - blk * a.block_size, a.block_size);
-    if (id >= a.num_blocks)
-        return;
-    const uint32_t r = divide(threadIdx.x, a.by_chunk), mine = threadIdx.x - r * a.by_chunk.d;
     const uint32_t chunk = slice * kThreads + mine;
-    const bool in = r < a.rows && chunk < a.slot_chunks;
+    const bool in = r < a.rows && chunk < a.slot_chunks && id < a.num_blocks &&
+                    (!SIDE || (beside < a.side && group * a.side + beside < a.blocks));
     const uint8_t *row = reinterpret_cast<const uint8_t *>(table_entry(a.tab, layer)) +
-                         static_cast<uint64_t>(id) * a.tile_bytes + (in ? chunk : 0u) * 16u;
+                         (in ? static_cast<uint64_t>(id) * a.tile_bytes + chunk * 16u : 0u);
     float lo[8], up[8];
     for (uint32_t t = in ? r : 0u, first = 1; t < held || first; t += 8u * a.rows) {
         u32x4 x[8];
@@ -90,12 +95,12 @@ __global__ void __launch_bounds__(kThreads) key_bounds_rows(const BoundsArgs a)
         part[0][threadIdx.x] = pack8<BF16>(lo);
         part[1][threadIdx.x] = pack8<BF16>(up);
         __syncthreads();
-        if (r > 0)
+        if (r > 0 || !in)
             return;
         for (uint32_t k = 1; k < a.rows; ++k) {
             float f[8], h[8];
-            unpack8<BF16>(part[0][k * a.by_chunk.d + mine], f);
-            unpack8<BF16>(part[1][k * a.by_chunk.d + mine], h);
+            unpack8<BF16>(part[0][threadIdx.x + k * a.by_chunk.d], f);
+            unpack8<BF16>(part[1][threadIdx.x + k * a.by_chunk.d], h);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 lo[e] = less_of(lo[e], f[e]);
@@ -108,6 +113,14 @@ __global__ void __launch_bounds__(kThreads) key_bounds_rows(const BoundsArgs a)
     const uint64_t at = (static_cast<uint64_t>(id) * a.slot_chunks + chunk) * 16u;
     *(LLMIG_GLOBAL u32x4 *)(table_entry(a.bounds_tab, layer) + at) = pack8<BF16>(lo);
     *(LLMIG_GLOBAL u32x4 *)(table_entry(a.bounds_tab, a.num_layers + layer) + at) = pack8<BF16>(up);
+}
+
+inline const void *key_bounds_kernel(int bf16, bool side)
+{
+    return bf16 ? side ? reinterpret_cast<const void *>(&key_bounds_rows<1, 1>)
+                       : reinterpret_cast<const void *>(&key_bounds_rows<1, 0>)
+           : side ? reinterpret_cast<const void *>(&key_bounds_rows<0, 1>)
+                  : reinterpret_cast<const void *>(&key_bounds_rows<0, 0>);
 }
 
 // ---------------------------------------------------------------------------
@@ -507,12 +520,14 @@ __global__ void __launch_bounds__(T) list_blocks(const SelectArgs a)
 
 // The kernel for rows of at most `longest` blocks, and its threads.  384 rows of up
 // to 4096 blocks, 256 / 512 / 1024 threads 16.4 / 12.4 / 11.9 us; 24 of up to 563 take
-// 5.6 with 256.
+// 5.6 with 256.  More keys a thread than a row needs cost time: 5 rows of 5829 blocks, 8 /
+// 16 of them 8.9 / 12.6 us.
 inline const void *list_kernel(uint32_t longest, uint32_t *threads)
 {
     *threads = longest <= 1024 ? 256 : 1024;
     return longest <= 1024    ? reinterpret_cast<const void *>(&list_blocks<256, 4>)
            : longest <= 4096  ? reinterpret_cast<const void *>(&list_blocks<1024, 4>)
+           : longest <= 8192  ? reinterpret_cast<const void *>(&list_blocks<1024, 8>)
            : longest <= 16384 ? reinterpret_cast<const void *>(&list_blocks<1024, 16>)
                               : reinterpret_cast<const void *>(&list_blocks<1024, 0>);
 }

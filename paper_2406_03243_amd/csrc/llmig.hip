@@ -1161,13 +1161,14 @@ struct AttnMigration {
 // Launches the partial kernel `fn` of a checked call over partitions of at
 // most `part` tokens.  a (zeroed but for what its mode adds) is filled in, and
 // r with the sequences that leave records: those of several partitions, or
-// (all_records) every one; returns the most partitions of one of them.
+// (all_records) every one; returns the most partitions of one of them.  lone: the
+// kernel whose wavefronts take a KV head each, for calls that attn_lone_heads picks.
 // Allocates nothing.
 template <class Args>
 static int attn_launch(Args &a, AttnReduceArgs &r, uint32_t *most_parts, const llmig_pool *pool, const void *fn,
                        const void *q, int32_t batch, int32_t q_heads, const int32_t *tables, int32_t table_stride,
                        const int32_t *ctx_lens, float scale, int32_t part, float *ws, float *out, hipStream_t st,
-                       const AttnMigration &mig, bool all_records)
+                       const AttnMigration &mig, bool all_records, const void *lone = nullptr)
 {
     constexpr bool kListed = std::is_same<Args, AttnListedArgs>::value;
     a.mig_seq = -1;
@@ -1193,7 +1194,6 @@ static int attn_launch(Args &a, AttnReduceArgs &r, uint32_t *most_parts, const l
     a.block_size = static_cast<uint32_t>(pool->block_size);
     a.table_stride = static_cast<uint32_t>(table_stride);
     a.part_tokens = static_cast<uint32_t>(part);
-    const uint64_t per_item = static_cast<uint64_t>(a.kv_heads) * a.num_layers;
     int64_t tokens = 0;
     int32_t longest = 0;
     for (int32_t b = 0; b < batch; ++b) {
@@ -1201,7 +1201,9 @@ static int attn_launch(Args &a, AttnReduceArgs &r, uint32_t *most_parts, const l
         longest = std::max(longest, ctx_lens[b]);
     }
     const int64_t n_items = attn_items(ctx_lens, batch, part);
-    const int64_t workgroups = n_items * static_cast<int64_t>(per_item);
+    const int64_t workgroups = n_items * static_cast<int64_t>(a.kv_heads) * a.num_layers;
+    const bool alone = lone && attn_lone_heads(workgroups, longest, pool->num_kv_heads);
+    const uint64_t per_item = static_cast<uint64_t>(alone ? (a.kv_heads + 3) / 4 : a.kv_heads) * a.num_layers;
     // launch order: several partitions first, longest partition first; a
     // sequence launched apart before the others (several partitions stay first)
     const bool apart = mig.dst && batch > 1 && attn_carry_apart(workgroups, tokens / n_items) &&
@@ -1236,7 +1238,7 @@ static int attn_launch(Args &a, AttnReduceArgs &r, uint32_t *most_parts, const l
     size_t lds = pool->block_size % 8 == 0
                      ? 0
                      : attn_blk_slots(a.part_tokens, a.block_size) * sizeof(int32_t) * (mig.dst || kListed ? 2 : 1);
-    const int per_cu = attn_workgroups_per_cu(pool->head_dim, workgroups, tokens / n_items, mig.dst != nullptr);
+    const int per_cu = alone ? 0 : attn_workgroups_per_cu(pool->head_dim, workgroups, tokens / n_items, mig.dst != nullptr);
     const bool by_layer = attn_layer_by_layer(pool->head_dim, workgroups, tokens / n_items);
     lds = std::max(lds, attn_spare_lds(pool->head_dim, per_cu));
     const uint32_t step = static_cast<uint32_t>(std::max<uint64_t>(kMaxGridWorkgroups / per_item, 1u));
@@ -1246,7 +1248,7 @@ static int attn_launch(Args &a, AttnReduceArgs &r, uint32_t *most_parts, const l
         a.item_base = at;
         a.layer_items = by_layer && !(mig.dst && at < carried) ? here : 0u;
         void *args[] = {&a};
-        hipError_t e = hipLaunchKernel(at < carried ? fn : mig.plain, dim3(static_cast<uint32_t>(here * per_item)),
+        hipError_t e = hipLaunchKernel(alone ? lone : at < carried ? fn : mig.plain, dim3(static_cast<uint32_t>(here * per_item)),
                                        dim3(kThreads), args, lds, st);
         if (e != hipSuccess)
             return hip_error(e);
@@ -1526,7 +1528,7 @@ int llmig_append_rotary(const llmig_pool *pool, const llmig_append_desc *d, void
     const int64_t L = pool->num_layers, bs = pool->block_size, D = pool->head_dim;
     AppendArgs a;
     std::memset(&a, 0, sizeof(a));
-    int64_t n = 0, most = 0;
+    int64_t n = 0, blocks = 0;      // tokens, and blocks that get some
     for (int32_t b = 0; b < d->batch; ++b) {
         const int64_t from = d->from_toks[b], add = d->n_toks[b], pos = d->first_pos ? d->first_pos[b] : from;
         if (from < 0 || add < 0 || pos < 0 || from + add > 0x7fffffffLL)
@@ -1537,7 +1539,7 @@ int llmig_append_rotary(const llmig_pool *pool, const llmig_append_desc *d, void
         n += add;
         if (n > 0x7fffffffLL / L)
             return LLMIG_EINVAL;
-        most = std::max(most, add);
+        blocks += add > 0 ? (from + add - 1) / bs - from / bs + 1 : 0;
         a.one_each = b == 0 ? add == 1 : a.one_each && add == 1;
         a.from[b] = d->from_toks[b];
         a.pos[b] = static_cast<int32_t>(pos);
@@ -1593,7 +1595,7 @@ int llmig_append_rotary(const llmig_pool *pool, const llmig_append_desc *d, void
     // layout whose tokens' rows do not lie in one piece
     bool by_blocks[2];
     for (int k = 0; k < 2; ++k)
-        by_blocks[k] = most >= kAppendBlockTokens && (pool->layouts[k] == LLMIG_LAYOUT_HCNX ||
+        by_blocks[k] = append_by_blocks(n, blocks, 4 * n * L * row[1]) && (pool->layouts[k] == LLMIG_LAYOUT_HCNX ||
                                                       (pool->layouts[k] == LLMIG_LAYOUT_HDN && bs % 8 == 0 && bs / 8 <= kThreads));
     a.rows_heads[0] = a.q_heads;
     a.rows_heads[1] = by_blocks[0] ? 0 : a.kv_heads;
@@ -1622,7 +1624,7 @@ int llmig_append_rotary(const llmig_pool *pool, const llmig_append_desc *d, void
     }
     if (!by_blocks[0] && !by_blocks[1])
         return LLMIG_OK;
-    int64_t blocks = 0;
+    blocks = 0;
     for (int32_t b = 0; b < d->batch; ++b) {
         if (d->n_toks[b] > 0)
             blocks += (static_cast<int64_t>(d->from_toks[b]) + d->n_toks[b] - 1) / bs - d->from_toks[b] / bs + 1;
@@ -1698,14 +1700,15 @@ int llmig_key_bounds(const llmig_pool *pool, const llmig_pool *bounds, int32_t d
     a.batch = static_cast<uint32_t>(batch);
     a.blocks = static_cast<uint32_t>(n);
     const uint32_t chunks = std::min(a.slot_chunks, static_cast<uint32_t>(kThreads));
-    a.rows = std::min(kThreads / chunks, a.block_size);
+    a.rows = std::min(kThreads / chunks, (a.block_size + 7) / 8);
+    a.side = kThreads / chunks / a.rows;
+    const uint32_t groups = (a.blocks + a.side - 1) / a.side;
     a.by_slice = divisor(slices);
-    a.by_block = divisor(a.blocks);
+    a.by_group = divisor(groups);
     a.by_chunk = divisor(chunks);
-    const void *fn = dtype ? reinterpret_cast<const void *>(&key_bounds_rows<1>)
-                           : reinterpret_cast<const void *>(&key_bounds_rows<0>);
-    return launch_items(fn, &a, static_cast<uint64_t>(n) * pool->num_layers * slices, 1, &a.first_item,
-                        static_cast<hipStream_t>(stream));
+    a.by_row = divisor(a.rows);
+    return launch_items(key_bounds_kernel(dtype, a.side > 1), &a, static_cast<uint64_t>(groups) * pool->num_layers * slices, 1,
+                        &a.first_item, static_cast<hipStream_t>(stream));
 }
 
 int llmig_select_blocks_workspace(const llmig_pool *bounds, int32_t block_size, const int32_t *ctx_lens,
@@ -1835,7 +1838,10 @@ int llmig_decode_attention_blocks(const llmig_pool *pool, int32_t dtype, const v
     AttnReduceArgs r;
     uint32_t most = 0;
     rc = attn_launch(a, r, &most, pool, fn, q, batch, q_heads, tables, table_stride, lens, scale, part,
-                     static_cast<float *>(workspace), out, static_cast<hipStream_t>(stream), AttnMigration(), false);
+                     static_cast<float *>(workspace), out, static_cast<hipStream_t>(stream), AttnMigration(), false,
+                     pool->block_size % 8 == 0
+                         ? attn_kernel_for(dtype, pool->head_dim, q_heads / pool->num_kv_heads, kAttnListed, 2)
+                         : nullptr);
     return rc == LLMIG_OK ? attn_merge(r, most, static_cast<hipStream_t>(stream)) : rc;
 }
 
@@ -1926,7 +1932,10 @@ int llmig_decode_attention_prefix(const llmig_pool *pool, int32_t dtype, const v
     uint32_t most = 0;
     float *own = static_cast<float *>(workspace) + p.prefix_bytes / 4;
     rc = attn_launch(o, r, &most, pool, fn, q, batch, q_heads, tables, table_stride, p.own, scale, p.part, own, out, st,
-                     AttnMigration(), true);
+                     AttnMigration(), true,
+                     pool->block_size % 8 == 0
+                         ? attn_kernel_for(dtype, pool->head_dim, q_heads / pool->num_kv_heads, kAttnOwn, 2)
+                         : nullptr);
     if (rc != LLMIG_OK)
         return rc;
     j.prefix = static_cast<const float *>(workspace);

@@ -129,6 +129,28 @@ def test_layouts(layouts, bs):
     run(L=1, H=1, G=1, D=128, bs=bs, dtype="fp16", froms=(8, 1), news=(16, 8), rotary=128, layouts=layouts)
 
 
+# prompts large enough to go block by block where a layout scatters their tokens
+BIG = dict(L=3, H=8, G=1, D=128, froms=(0, 7, 31, 5), news=(300, 129, 150, 1), rotary=128)
+
+
+@pytest.mark.parametrize("layouts", [(2, 3), (3, 2), (0, 3), (2, 0)])
+@pytest.mark.parametrize("bs,interleaved,rotary", [(8, False, 128), (16, True, 128), (16, False, 64), (32, False, 24),
+                                                   (16, True, 2), (64, False, 0)])
+def test_prompts_block_by_block(layouts, bs, interleaved, rotary):
+    run(**dict(BIG, rotary=rotary), bs=bs, interleaved=interleaved, layouts=layouts)
+
+
+@pytest.mark.parametrize("bs", [4, 12, 24, 40])
+def test_prompts_block_by_block_of_odd_sizes(bs):
+    run(**dict(BIG, L=2, H=13, D=104, rotary=104, news=(400, 129, 150, 2)), bs=bs, dtype="fp16", layouts=(2, 3))
+    run(**dict(BIG, L=30, H=1, D=80, rotary=80, news=(900, 129, 400, 2)), bs=bs, layouts=(3, 2), with_q=False, table_offset=1)
+
+
+def test_many_layers_block_by_block():
+    """Units enough for two layers a workgroup, an odd number of layers."""
+    run(**dict(BIG, L=41, H=2, D=64, rotary=64), layouts=(2, 3))
+
+
 @pytest.mark.parametrize("bs", [1, 4, 12])
 def test_odd_blocks(bs):
     run(bs=bs, froms=(0, 11), news=(13, 30))
@@ -166,14 +188,14 @@ def test_values_keep_their_bits():
     NaN payloads and subnormals among them."""
     g = np.random.default_rng(3)
     bits = lambda shape: torch.from_numpy(g.integers(-32768, 32768, size=tuple(shape)).astype(np.int16))
-    for layouts in ((0, 0), (2, 3), (1, 1)):
-        gk, gv, q_out, k, v, q = run(H=2, D=128, rotary=64, froms=(0,), news=(40,), layouts=layouts, values=bits)
-        tables_free = gv.reshape(1, -1, 2, 128)        # slots in block order
-        want = {r.numpy().tobytes() for r in v.contiguous().view(torch.int16).reshape(-1, 2, 128)}
+    for layouts, H, news in (((0, 0), 2, 40), ((2, 3), 2, 40), ((1, 1), 2, 40), ((2, 3), 24, 530), ((3, 2), 24, 530)):
+        gk, gv, q_out, k, v, q = run(H=H, D=128, rotary=64, froms=(0,), news=(news,), layouts=layouts, values=bits)
+        tables_free = gv.reshape(1, -1, H, 128)        # slots in block order
+        want = {r.numpy().tobytes() for r in v.contiguous().view(torch.int16).reshape(-1, H, 128)}
         have = {r.numpy().tobytes() for r in tables_free.contiguous().view(torch.int16)[0]}
         assert want <= have
-        tail = {r.numpy().tobytes() for r in k.contiguous().view(torch.int16).reshape(-1, 2, 128)[:, :, 64:].contiguous()}
-        assert tail <= {r.numpy().tobytes() for r in gk.reshape(1, -1, 2, 128)[0, :, :, 64:].contiguous().view(torch.int16)}
+        tail = {r.numpy().tobytes() for r in k.contiguous().view(torch.int16).reshape(-1, H, 128)[:, :, 64:].contiguous()}
+        assert tail <= {r.numpy().tobytes() for r in gk.reshape(1, -1, H, 128)[0, :, :, 64:].contiguous().view(torch.int16)}
         assert torch.equal(q_out[..., 64:].contiguous().view(torch.int16), q[..., 64:].contiguous().view(torch.int16))
 
 

@@ -132,7 +132,7 @@ def test_equal_scores_go_to_the_first():
         choose(b, q, tables, [1600], 16, 0, 1, count)
 
 
-@pytest.mark.parametrize("blocks", [5000, 17000])
+@pytest.mark.parametrize("blocks", [5000, 9000, 17000])
 def test_equal_scores_of_long_rows(blocks):
     kv, q, tables, gen = make(1, 1, 1, 64, 1, "fp16", [blocks])
     b = random_bounds(kv, gen)
@@ -221,6 +221,18 @@ def test_attention_over_lists(order, holes, dtype, L, H, G, D, bs, ctx, count):
     print("[case]", order, dtype, L, H, G, D, bs, ctx, count, flush=True)
     kv, q, tables, gen = make(L, H, G, D, bs, dtype, ctx)
     attend(kv, q, tables, ctx, some_lists(L, len(ctx), H, count, ctx, bs, gen, order, holes), dtype)
+
+
+@pytest.mark.parametrize("order,holes", [("ascending", False), ("any", True)])
+@pytest.mark.parametrize("dtype,L,H,G,D,bs,B,longest", [
+    ("bf16", 2, 5, 2, 128, 16, 110, 90), ("fp16", 2, 4, 1, 64, 8, 140, 93), ("bf16", 8, 2, 16, 64, 32, 70, 77),
+    ("fp16", 4, 13, 1, 128, 16, 60, 260), ("bf16", 30, 3, 4, 128, 24, 75, 500)])
+def test_many_short_lists(order, holes, dtype, L, H, G, D, bs, B, longest):
+    """A wavefront walks the list of a KV head by itself; heads that four does not divide."""
+    print("[case]", order, dtype, L, H, G, D, bs, B, longest, flush=True)
+    ctx = [0, longest, 1] + [1 + (i * i * 7) % (longest if i < 20 else min(longest, 60)) for i in range(B - 3)]
+    kv, q, tables, gen = make(L, H, G, D, bs, dtype, ctx)
+    attend(kv, q, tables, ctx, some_lists(L, B, H, -(-longest // bs), ctx, bs, gen, order, holes), dtype)
 
 
 def test_a_block_listed_twice_counts_twice():

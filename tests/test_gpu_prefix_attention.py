@@ -122,6 +122,21 @@ def test_full_batch():
     run(*setup(1, 8, 1, 64, 16, "bf16", ctx, 19), ctx, 19, "bf16", once=True)
 
 
+# as those, with few tokens behind the prefix: a wavefront takes those of a KV head
+FEW = [
+    (2, 5, 1, 128, 16, "bf16", [700, 0, 41, 688, 770] + [688 + (i % 30) for i in range(110)], 43),
+    (3, 4, 2, 64, 8, "fp16", [731, 640, 12, 0] + [640 + (i * i) % 90 for i in range(96)], 80),
+    (5, 2, 4, 128, 24, "bf16", [480 + (i % 70) for i in range(128)], 20),
+]
+
+
+@pytest.mark.parametrize("case", FEW, ids=lambda c: f"L{c[0]}_H{c[1]}_G{c[2]}_D{c[3]}_bs{c[4]}_{c[5]}")
+def test_few_own_tokens_of_many(case):
+    print("[case]", case, flush=True)
+    L, H, G, D, bs, dtype, ctx, prefix = case
+    run(*setup(L, H, G, D, bs, dtype, ctx, prefix), ctx, prefix, dtype)
+
+
 # the batch of the tests below, and its prefix: rows of both halves of a product's
 # columns, three tiles, the last one partly filled
 CTX, PREFIX = [688 + (5 * i) % 13 for i in range(30)], 43

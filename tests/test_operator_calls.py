@@ -90,27 +90,28 @@ def test_calls_without_work_launch_nothing(call):
 
 
 def test_append_goes_block_by_block_where_tokens_are_scattered(call):
-    many, one = dict(n_toks=[2, 20]), dict(n_toks=[1, 1])
+    many, one = dict(n_toks=[2, 20000], positions=21000, table_stride=2600), dict(n_toks=[1, 1])
     paged = dict(layouts=(2, 3))
     for kw, want in [
             (dict(**many), ["append_rotary_rows"]), (dict(pool_args=dict(layouts=(1, 1)), **many), ["append_rotary_rows"]),
-            (dict(pool_args=paged, **one), ["append_rotary_rows"]),
+            (dict(pool_args=paged, **one), ["append_rotary_rows"]), (dict(pool_args=paged, n_toks=[2, 20]), ["append_rotary_rows"]),
             (dict(pool_args=paged, **many), ["append_rotary_rows", "append_rotary_slots", "append_rotary_dims"]),
             (dict(pool_args=paged, q_heads=0, **many), ["append_rotary_slots", "append_rotary_dims"]),
             (dict(pool_args=dict(layouts=(3, 2)), **many), ["append_rotary_rows", "append_rotary_dims", "append_rotary_slots"]),
             (dict(pool_args=dict(layouts=(3, 0)), **many), ["append_rotary_rows", "append_rotary_dims"]),
-            (dict(pool_args=dict(layouts=(0, 3), bs=12), table_stride=8, **many), ["append_rotary_rows"])]:
+            (dict(pool_args=dict(layouts=(0, 3), bs=12), **many), ["append_rotary_rows"])]:
         got = call([dict(op="append", **kw)])[0]
         assert got["rc"] == OK and kernels(got) == want, kw
 
 
 def test_select_scores_only_what_has_to_be_chosen_from(call):
-    few, many, long, longer, longest = call([
+    few, many, long, longer, longish, longest = call([
         dict(op="select", count=7, keep_first=0), dict(op="select"),
         dict(op="select", ctx_lens=[16 * 1025, 3], table_stride=2000), dict(op="select", ctx_lens=[16 * 4097, 3], table_stride=9000),
+        dict(op="select", ctx_lens=[16 * 8193, 3], table_stride=9000),
         dict(op="select", ctx_lens=[16 * 16385, 3], table_stride=20000)])
     assert kernels(few) == ["list_blocks"] and kernels(many) == ["score_blocks", "list_blocks"]
-    assert [x["launches"][-1]["template"] for x in (many, long, longer, longest)] == [[256, 4], [1024, 4], [1024, 16],
+    assert [x["launches"][-1]["template"] for x in (many, long, longer, longish, longest)] == [[256, 4], [1024, 4], [1024, 8], [1024, 16],
                                                                                       [1024, 0]]
 
 
@@ -130,10 +131,12 @@ def test_prefix_is_read_once_only_where_that_pays(call):
 
 def test_prefix_cases_of_the_gpu_tests_read_it_once(call):
     import test_gpu_prefix_attention as t
-    for L, H, G, D, bs, dtype, ctx, prefix in t.SHARED + [(*t.SHAPE, "bf16", t.CTX, t.PREFIX)]:
+    for L, H, G, D, bs, dtype, ctx, prefix in t.SHARED + t.FEW + [(*t.SHAPE, "bf16", t.CTX, t.PREFIX)]:
         got = call([dict(op="prefix", pool_args=dict(layers=L, blocks=2000, bs=bs, heads=H, dim=D), q_heads=H * G,
                          table_stride=max(ctx) // bs + 1, ctx_lens=ctx, prefix_blocks=prefix)])[0]
         assert got["rc"] == OK and kernels(got)[0] == "prefix_rows", (L, H, G, D, bs)
+        if (L, H, G, D, bs, dtype, ctx, prefix) in t.FEW:
+            assert got["launches"][1]["template"][3] == 2, (L, H, G, D, bs)
 
 
 def test_workspaces_are_those_of_the_records(call):
@@ -148,3 +151,16 @@ def test_workspaces_are_those_of_the_records(call):
                    table_stride=60)])[0]
     records = p["workspace"] // (16 * 132 * 4)
     assert p["workspace"] % (16 * 132 * 4) == 0 and records >= 60 and records % 30 == 0
+
+
+def test_short_sequences_take_a_wavefront_a_head(call):
+    shape = dict(pool_args=dict(layers=2, heads=8, dim=128), q_heads=32, table_stride=80)
+    many, longer = dict(batch=128, ctx_lens=[40] * 128), dict(batch=128, ctx_lens=[400] * 128)
+    got = call([dict(op="attend", **shape, **dict(batch=60, ctx_lens=[40] * 60)), dict(op="attend", **shape, **many),
+                dict(op="attend", count=64, **shape, **longer), dict(op="attend", **dict(shape, pool_args=dict(
+                    layers=16, heads=1, dim=128), q_heads=4), **many),
+                dict(op="attend", **dict(shape, pool_args=dict(layers=2, heads=8, dim=128, bs=12)), **many),
+                dict(op="prefix", ctx_lens=[1000] * 128, prefix_blocks=60, **shape)])
+    assert all(x["rc"] == OK for x in got)
+    kind = [[l["template"][3] for l in x["launches"] if l["kernel"] == "attn_partial_mfma"] for x in got]
+    assert kind == [[1], [2], [1], [1], [0], [2]]
