@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
     // own, so that the compiler sees which loads a read has to wait for.
     __shared__ __align__(16) uint8_t tile_a[2 * kTileBytes], tile_b[2 * kTileBytes];
     static_assert(4 * 16 * D * 4 <= 2 * kTileBytes, "the merge of 16 rows fits");
-    __shared__ float sh_m[4][32], sh_l[4][32];
+    __shared__ float sh_m[4][32], sh_l[4][32], sh_c[4][32];
 
     // The workgroups that read the same tokens (a partition's row chunks, then
     // its KV heads, whose rows adjoin) follow each other on one XCD.
@@ -364,50 +364,67 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
         work((t0 - t_begin) / T % 2u ? tile_b : tile_a, t0, std::true_type());
     }
 
-    // The wavefronts that split the tokens meet in LDS, 16 rows of each at a
-    // time, and the records leave in whole rows.
+    // The records leave in whole rows, through LDS, 16 rows of each wavefront at a
+    // time; wavefronts that split the tokens meet there.  (Chunk c of row r stands at
+    // c ^ r, so that what is written at once falls on distinct banks; G is a power of
+    // two.  With divisions by G, a row's factors found for each of its chunks and
+    // conflicts, this took 6 us of a workgroup's time, now 1.5.)
     lsum = sum_of_halves(lsum);
     if (half == 0) {
         sh_m[wave][l32] = m;
         sh_l[wave][l32] = lsum;
     }
     float *so = reinterpret_cast<float *>(tile_a);                // [wave][16 rows][D]
+    const uint32_t g_log = 31u - __builtin_clz(G);
+    float *recs = a.ws + ((static_cast<uint64_t>(layer) * a.parts + part) * a.members * a.q_heads + g * G) * (D + kAttnHeader);
+    auto record = [&](uint32_t row) {
+        return recs + static_cast<uint64_t>((row >> g_log) * a.q_heads + (row & (G - 1u))) * (D + kAttnHeader);
+    };
+    __syncthreads();
+    if (threadIdx.x < 32u * WM) {
+        const uint32_t w0 = threadIdx.x / 32u, rr = threadIdx.x % 32u, row = chunk * 32u * WM + threadIdx.x;
+        float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+        for (uint32_t w = 0; w < 4 / WM; ++w)
+            mm = fmaxf(mm, sh_m[w * WM + w0][rr]);
+#pragma unroll
+        for (uint32_t w = 0; w < 4 / WM; ++w) {
+            const float mw = sh_m[w * WM + w0][rr];
+            // (no weight: a factor of 1 would do as well, but for a NaN sum)
+            const float c = mw == -INFINITY ? 1.f : exp2f(mw - mm);
+            ll += sh_l[w * WM + w0][rr] * c;
+            sh_c[w * WM + w0][rr] = c;
+        }
+        if (row < M)              // the maximum in the natural base, as attn_partial_mfma leaves it
+            *(LLMIG_GLOBAL f32x4_t *)record(row) = f32x4_t{mm == -INFINITY ? -INFINITY : mm / kLog2e, ll, 0.f, 0.f};
+    }
 #pragma unroll
     for (uint32_t rt = 0; rt < 2; ++rt) {
-        __syncthreads();
+        if (rt > 0)
+            __syncthreads();
         if (l32 / 16u == rt) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    *reinterpret_cast<f32x4_t *>(so + (wave * 16u + r16) * D + 32 * mt + 8 * i + 4 * half) =
+                    *reinterpret_cast<f32x4_t *>(so + (wave * 16u + r16) * D + 4u * ((8u * mt + 2u * i + half) ^ r16)) =
                         f32x4_t{acc[mt][4 * i], acc[mt][4 * i + 1], acc[mt][4 * i + 2], acc[mt][4 * i + 3]};
         }
         __syncthreads();
-        for (uint32_t x = threadIdx.x; x < WM * 16u * (D / 4); x += kThreads) {
-            const uint32_t r = x / (D / 4), d4 = x % (D / 4), w0 = r / 16u, rr = r % 16u;
-            const uint32_t row = chunk * 32u * WM + w0 * 32u + 16u * rt + rr;
-            if (row >= M)
-                continue;
-            float mm = -INFINITY, ll = 0.f;
+        constexpr uint32_t kRows = kThreads / (D / 4);                // rows stored at a time
+        const uint32_t d4 = threadIdx.x % (D / 4), r0 = threadIdx.x / (D / 4);
 #pragma unroll
-            for (uint32_t w = 0; w < 4 / WM; ++w)
-                mm = fmaxf(mm, sh_m[w * WM + w0][16 * rt + rr]);
+        for (uint32_t k = 0; k < WM * 16u / kRows; ++k) {
+            const uint32_t r = k * kRows + r0, w0 = r / 16u, rr = r % 16u, row = chunk * 32u * WM + w0 * 32u + 16u * rt + rr;
             f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (uint32_t w = 0; w < 4 / WM; ++w) {
                 const uint32_t v = w * WM + w0;
-                const float mw = sh_m[v][16 * rt + rr];
-                // (no weight: a factor of 1 would do as well, but for a NaN sum)
-                const float c = mw == -INFINITY ? 1.f : exp2f(mw - mm);
-                ll += sh_l[v][16 * rt + rr] * c;
-                o += *reinterpret_cast<const f32x4_t *>(so + (v * 16u + rr) * D + 4 * d4) * c;
+                const f32x4_t x = *reinterpret_cast<const f32x4_t *>(so + (v * 16u + rr) * D + 4u * (d4 ^ rr));
+                o = WM == 4 ? x : o + x * sh_c[v][16 * rt + rr];
             }
-            float *rec = a.ws + (((static_cast<uint64_t>(layer) * a.parts + part) * a.members + row / G) * a.q_heads + g * G +
-                                 row % G) * (D + kAttnHeader);
-            *(LLMIG_GLOBAL f32x4_t *)(rec + kAttnHeader + 4 * d4) = o;
-            if (d4 == 0)          // the maximum in the natural base, as attn_partial_mfma leaves it
-                *(LLMIG_GLOBAL f32x4_t *)rec = f32x4_t{mm == -INFINITY ? -INFINITY : mm / kLog2e, ll, 0.f, 0.f};
+            if (row < M)
+                *(LLMIG_GLOBAL f32x4_t *)(record(row) + kAttnHeader + 4 * d4) = o;
         }
     }
 }
