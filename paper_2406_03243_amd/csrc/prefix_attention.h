@@ -541,13 +541,13 @@ struct PrefixCut {
 };
 
 // Partitions fill the chip, two workgroups a CU; each costs a record per row,
-// written and read again.  What a cut takes was measured for 18 shapes (1 to 32
-// layers, 4 to 32 heads, 8 to 512 rows, prefixes of 512 to 16384 tokens, 1 to 64
-// partitions) and is, in rounds of 512 workgroups,
+// written and read again.  What a cut takes was measured for 31 shapes (1 to 33
+// layers, 4 to 32 heads, 6 to 512 rows, prefixes of 128 to 16384 tokens, 1 to 64
+// partitions) and is, in rounds of 512 workgroups, beyond what all cuts take,
 //     3 us + tiles of a partition x 1.4 us (x 1.6 with two a CU) + 0.35 ns a record,
-// for head_dim 128: the partitions that this puts first were within 1.4% of the
-// best ones on average, 7.4% at most (8 heads, 512 rows, 8192 tokens: 1 partition
-// 231 us, 4 76, 8 53.6, 12 58, 32 74).
+// for head_dim 128: the partitions that this puts first were within 1.2% of the
+// best ones on average, 7.9% at most (8 heads, 512 rows, 8192 tokens: 1 partition
+// 207 us, 4 68, 8 49, 12 52, 32 69).
 constexpr int64_t kPrefixStartNs = 3000, kPrefixTileNs = 1400;
 constexpr uint32_t kPrefixMostParts = 128;
 
@@ -583,17 +583,20 @@ inline PrefixCut prefix_cut(uint32_t rows, int64_t tokens, int64_t layer_heads, 
 // attention, and every row leaves a record of its own tokens, too.  Plain attention
 // reads the prefix for each of `members` sequences, after the first mostly out of
 // the caches: 10 to 14 TB/s where an XCD's share of the layers fits into its L2,
-// 7 to 10 else.  Prefix / plain, us: one layer of 8 heads of 128 and 4 query heads
-// each, 7 sequences behind 2000 tokens 18.0 / 15.7, 8 behind 8192 23 / 32, 64 behind
-// 512 23.5 / 17.8; 8 query heads each, 32 behind 2000 33 / 30, 64 behind 2000 36 / 74;
-// 8 layers, 32 behind 128 34 / 22, 8 behind 512 20 / 17, 32 behind 512 40 / 48, 8
-// behind 2000 28 / 70.
+// 7 to 10 else; and a workgroup of its own costs more than the quarter of one that
+// a short rest of a sequence takes.  Prefix / plain, us: one layer of 8 heads of 128
+// and 4 query heads each, 7 sequences behind 2000 tokens 17.1 / 14.8, 8 behind 8192
+// 22.7 / 31.6, 64 behind 512 21.0 / 18.0; 8 query heads each, 16 behind 2000 24.0 /
+// 22.9, 64 behind 2000 31 / 73; 8 layers, 16 behind 512 24.4 / 25.4, 8 behind 2000 27 /
+// 68; 9 layers of 32 heads, 8 behind 160 30 / 42.
 inline bool prefix_pays(const PrefixCut &c, int64_t members, int64_t group, int64_t tokens, int64_t layers, int64_t heads,
                         int64_t head_dim)
 {
     const double layer_bytes = static_cast<double>(tokens) * heads * head_dim * 4;
     const bool cached = layer_bytes * std::max<int64_t>(1, layers / 8) <= 4 << 20;
-    const double plain_ns = layer_bytes * layers * members / (cached ? 12500. : 8500.);
+    const double workgroups = static_cast<double>(layers) * heads * members;
+    const double plain_ns = layer_bytes * layers * members / (cached ? 12500. : 8500.) +
+                            (workgroups >= 1024 ? 3.5 * workgroups : 0.);
     return c.ns + 6500 + members * group * layers * heads * head_dim * 35 / 12800 < plain_ns;
 }
 
