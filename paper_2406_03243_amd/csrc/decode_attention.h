@@ -83,10 +83,15 @@ struct AttnListedArgs : AttnArgs {
 };
 
 // The tokens behind a shared prefix (MODE kAttnOwn): ctx counts those alone,
-// and the tables of the sequences whose bit is set start skip blocks later.
+// and the tables of the sequences whose bit is set start skip blocks later.  Such a
+// sequence (number b in the batch) is the place[b]-th one behind the prefix.
 struct AttnOwnArgs : AttnArgs {
+    const float *prefix;        // records [L][prefix_parts][members][Hq][D + kAttnHeader]
+    uint32_t prefix_parts, members;
+    uint32_t joins;             // 0: every item leaves a record
     uint32_t skip;
     uint32_t behind[kAttnMaxBatch / 32];
+    uint8_t place[kAttnMaxBatch];
 };
 
 struct AttnReduceArgs {
@@ -391,7 +396,9 @@ constexpr float attn_weights_up(int bf16)
 //               140 us, 5.8 TB/s; of 64 blocks of 3 requests, one layer, 9 us, a chain
 //               of list, table, rows, products and merge.
 //  kAttnOwn     the tokens of each sequence behind a prefix that prefix_rows
-//               (prefix_attention.h) computes: every item leaves a record.
+//               (prefix_attention.h) computes.  A sequence of one partition joins
+//               the prefix's records with its own sums, if they are few; others
+//               leave records.
 //               40 requests, 8 layers of 32 heads, 686 MB in 120 us, 5.7 TB/s.
 enum AttnMode { kAttnPlain = 0, kAttnMigrating = 1, kAttnListed = 2, kAttnOwn = 3 };
 
@@ -828,7 +835,9 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
     __syncthreads();
     // the sequence's output if it is one partition, else a record; of the
     // group's query heads
-    const bool whole = MODE != kAttnOwn && parts == 1;
+    bool whole = parts == 1;
+    if constexpr (MODE == kAttnOwn)
+        whole = whole && a.joins;
     const uint32_t out_row = whole ? D : D + kAttnHeader, out_at = whole ? 0u : kAttnHeader;
     const uint64_t out_first = whole ? static_cast<uint64_t>(layer) * a.batch + b
                                      : static_cast<uint64_t>(layer) * a.n_records + item;
@@ -854,6 +863,34 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
             const float c = mm == -INFINITY ? 0.f : exp2f(sh_m[w][row] - mm);
             ll += sh_l[w][row] * c;
             o += *reinterpret_cast<const f32x4_t *>(so + (w * 16 + row) * kMergeRow + 4 * d4) * c;
+        }
+        if constexpr (MODE == kAttnOwn) {
+            const uint32_t shared = whole && (a.behind[b / 32u] >> (b % 32u) & 1u) ? a.prefix_parts : 0u;
+            const float *rec = a.prefix + ((static_cast<uint64_t>(layer) * a.prefix_parts * a.members + a.place[b]) * a.q_heads +
+                                           g * G + row) * (D + kAttnHeader);
+            const uint64_t rec_step = static_cast<uint64_t>(a.members) * a.q_heads * (D + kAttnHeader);
+            for (uint32_t p0 = 0; p0 < shared; p0 += 8) {
+                float2 ml[8];
+                f32x4_t v[8];
+#pragma unroll
+                for (uint32_t u = 0; u < 8; ++u) {          // (past the end: no weight)
+                    const float *at = rec + min(p0 + u, shared - 1u) * rec_step;
+                    ml[u] = *reinterpret_cast<const float2 *>(at);
+                    v[u] = *reinterpret_cast<const f32x4_t *>(at + kAttnHeader + 4 * d4);
+                }
+#pragma unroll
+                for (uint32_t u = 0; u < 8; ++u) {
+                    if (p0 + u >= shared)
+                        break;
+                    const float m2 = ml[u].x * kLog2e, m_new = fmaxf(mm, m2);
+                    // (no weight on either side: factors of 1, so that a NaN sum stays one)
+                    const float c1 = m_new == -INFINITY ? 1.f : exp2f(mm - m_new);
+                    const float c2 = m_new == -INFINITY ? 1.f : exp2f(m2 - m_new);
+                    ll = ll * c1 + ml[u].y * c2;
+                    o = o * c1 + v[u] * c2;
+                    mm = m_new;
+                }
+            }
         }
         if (whole)                  // as the merge kernel: zeros where there is no finite weight sum
             o = ll > 0.f ? o / ll : f32x4_t{0.f, 0.f, 0.f, 0.f};

@@ -1502,12 +1502,18 @@ static int prefix_plan(const llmig_pool *pool, const int32_t *ctx_lens, int32_t 
     for (int32_t b = 0; b < batch; ++b)
         p->own[b] = p->members && ctx_lens[b] >= tokens ? static_cast<int32_t>(ctx_lens[b] - tokens) : ctx_lens[b];
     p->part = attn_part_tokens(p->own, batch, L, H, D);
-    if (!p->members)
-        return attn_record_bytes(p->own, batch, p->part, L, q_heads, D, &p->own_bytes);
+    if (!p->members || prefix_joins(p->cut.parts)) {
+        const int rc = attn_record_bytes(p->own, batch, p->part, L, q_heads, D, &p->own_bytes);
+        if (rc != LLMIG_OK || !p->members)
+            return rc;
+    } else {
+        int64_t n = 0;
+        if (__builtin_mul_overflow(attn_items(p->own, batch, p->part), L * q_heads, &n) ||
+            __builtin_mul_overflow(n, (D + kAttnHeader) * 4, &p->own_bytes))
+            return LLMIG_EINVAL;
+    }
     int64_t v = 0;
-    if (__builtin_mul_overflow(attn_items(p->own, batch, p->part), L * q_heads, &v) ||
-        __builtin_mul_overflow(v, (D + kAttnHeader) * 4, &p->own_bytes) ||
-        __builtin_mul_overflow(static_cast<int64_t>(p->cut.parts) * p->members, L * q_heads, &v) ||
+    if (__builtin_mul_overflow(static_cast<int64_t>(p->cut.parts) * p->members, L * q_heads, &v) ||
         __builtin_mul_overflow(v, (D + kAttnHeader) * 4, &p->prefix_bytes) ||
         p->prefix_bytes > INT64_MAX - p->own_bytes)
         return LLMIG_EINVAL;
@@ -1887,9 +1893,8 @@ int llmig_decode_attention_prefix(const llmig_pool *pool, int32_t dtype, const v
                                                   pool->block_size % 8 == 0),
                             q, batch, q_heads, tables, table_stride, ctx_lens, scale, static_cast<float *>(workspace),
                             workspace_bytes, out, st);
-    const uint64_t rows = static_cast<uint64_t>(pool->num_layers) * batch * q_heads;
     const uint64_t grid = static_cast<uint64_t>(pool->num_layers) * p.cut.parts * pool->num_kv_heads * p.cut.chunks;
-    if (rows > 0x7fffffffull || grid > kMaxGridWorkgroups)
+    if (static_cast<uint64_t>(pool->num_layers) * batch * q_heads > 0x7fffffffull || grid > kMaxGridWorkgroups)
         return LLMIG_EINVAL;
     PrefixArgs a;
     std::memset(&a, 0, sizeof(a));
@@ -1918,26 +1923,29 @@ int llmig_decode_attention_prefix(const llmig_pool *pool, int32_t dtype, const v
         return hip_error(e);
     AttnOwnArgs o;
     std::memset(&o, 0, sizeof(o));
+    o.prefix = a.ws;
+    o.prefix_parts = a.parts;
+    o.members = a.members;
+    o.joins = prefix_joins(a.parts);
     o.skip = static_cast<uint32_t>(prefix_blocks);
-    PrefixJoinArgs j;
-    std::memset(&j, 0, sizeof(j));
-    uint16_t place[kAttnMaxBatch];
-    for (int32_t b = 0; b < batch; ++b)
-        place[b] = static_cast<uint16_t>(p.members);
     for (uint32_t k = 0; k < p.members; ++k) {
         o.behind[p.member[k] / 32] |= 1u << (p.member[k] % 32);
-        place[p.member[k]] = static_cast<uint16_t>(k);
+        o.place[p.member[k]] = static_cast<uint8_t>(k);
     }
     AttnReduceArgs r;
     uint32_t most = 0;
     float *own = static_cast<float *>(workspace) + p.prefix_bytes / 4;
     rc = attn_launch(o, r, &most, pool, fn, q, batch, q_heads, tables, table_stride, p.own, scale, p.part, own, out, st,
-                     AttnMigration(), true,
+                     AttnMigration(), !o.joins,
                      pool->block_size % 8 == 0
                          ? attn_kernel_for(dtype, pool->head_dim, q_heads / pool->num_kv_heads, kAttnOwn, 2)
                          : nullptr);
     if (rc != LLMIG_OK)
         return rc;
+    if (r.seqs == 0)
+        return LLMIG_OK;
+    PrefixJoinArgs j;
+    std::memset(&j, 0, sizeof(j));
     j.prefix = static_cast<const float *>(workspace);
     j.own = own;
     j.out = out;
@@ -1947,11 +1955,14 @@ int llmig_decode_attention_prefix(const llmig_pool *pool, int32_t dtype, const v
     j.parts = a.parts;
     j.members = a.members;
     j.n_records = r.n_records;
-    for (int32_t s = 0; s < batch; ++s) {
+    j.seqs = r.seqs;
+    for (uint32_t s = 0; s < r.seqs; ++s) {
+        const uint32_t b = r.seq[s];
         j.seq_end[s] = r.seq_end[s];
         j.seq[s] = r.seq[s];
-        j.member[s] = place[r.seq[s]];
+        j.member[s] = o.behind[b / 32] >> (b % 32) & 1u ? o.place[b] : static_cast<uint16_t>(p.members);
     }
+    const uint64_t rows = static_cast<uint64_t>(j.num_layers) * j.seqs * j.q_heads;
     uint32_t per = 0;
     const void *jfn = prefix_join_kernel(pool->head_dim, rows, most + p.cut.parts, &per);
     for (uint64_t at = 0; at < rows; at += static_cast<uint64_t>(kMaxGridWorkgroups) * per) {

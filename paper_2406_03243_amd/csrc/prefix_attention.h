@@ -6,9 +6,10 @@
 // each KV head, attend to the same K and V, which are read once for all of
 // them: S = K Q^T and O = V^T P^T are products of M columns.  prefix_rows cuts
 // the prefix into partitions and leaves a record (maximum, weight sum,
-// weighted V sum) per partition and row; attn_partial_mfma leaves the records
-// of each sequence's own tokens (decode_attention.h, kAttnOwn), and prefix_join
-// joins both by the maxima.
+// weighted V sum) per partition and row; attn_partial_mfma (decode_attention.h,
+// kAttnOwn) takes each sequence's own tokens and joins both by the maxima, or, of
+// own tokens cut into several partitions and of many partitions of the prefix,
+// leaves records for prefix_join.
 #pragma once
 
 #include "append_rotary.h"
@@ -39,8 +40,9 @@ struct PrefixJoinArgs {
     const float *prefix, *own;   // records
     float *out;                  // [L][B][Hq][D]
     uint32_t num_layers, batch, q_heads, parts, members, n_records;
+    uint32_t seqs;               // sequences that left records
     uint32_t row_base;           // this launch's first row
-    uint32_t seq_end[kAttnMaxBatch];      // own records of the first s + 1 sequences
+    uint32_t seq_end[kAttnMaxBatch];      // own records of the first s + 1 of them
     uint16_t member[kAttnMaxBatch];       // sequence s's place among the members (members: none)
     uint8_t seq[kAttnMaxBatch];           // its number in the batch
 };
@@ -429,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
     }
 }
 
-// Joins the records of the prefix and of a sequence's own tokens; bound by reading
+// Joins the records of the prefix and of own tokens that left some; bound by reading
 // them (40 sequences of 32 heads of 128, 8 layers, 6.5 us).  D / 4 lanes
 // a row (layer, sequence, query head) and record, SUB of them side by side, each
 // with every SUB-th record, eight records' loads in flight; they meet in LDS.
@@ -438,10 +440,10 @@ __global__ void __launch_bounds__(kThreads) prefix_join(const PrefixJoinArgs a)
 {
     constexpr uint32_t kQuads = D / 4, kRec = D + kAttnHeader, kRows = kThreads / (kQuads * SUB);
     const uint32_t d4 = threadIdx.x % kQuads, sub = threadIdx.x / kQuads % SUB, mine = threadIdx.x / (kQuads * SUB);
-    const uint32_t rows = a.num_layers * a.batch * a.q_heads;
+    const uint32_t rows = a.num_layers * a.seqs * a.q_heads;
     const uint32_t r0 = a.row_base + blockIdx.x * kRows + mine;
     const uint32_t r = min(r0, rows - 1u);
-    const uint32_t h = r % a.q_heads, s = r / a.q_heads % a.batch, layer = r / a.q_heads / a.batch;
+    const uint32_t h = r % a.q_heads, s = r / a.q_heads % a.seqs, layer = r / a.q_heads / a.seqs;
     const uint32_t first = s > 0 ? a.seq_end[s - 1] : 0u;
     const uint32_t place = a.member[s], shared = place < a.members ? a.parts : 0u;
     const uint32_t all = shared + a.seq_end[s] - first;
@@ -532,6 +534,19 @@ inline const void *prefix_kernel_for(int bf16, int head_dim, uint32_t wm, bool a
     return bf16 ? prefix_kernel<1, 128>(wm, aligned) : prefix_kernel<0, 128>(wm, aligned);
 }
 
+// Whether the workgroups of the own tokens join the records of so many partitions
+// themselves.  It saves a launch and a record per row, but one workgroup reads the
+// partitions of its rows in turns of eight, which prefix_join reads side by side.
+// Joined / left to prefix_join, us: 2 layers of 8 heads, 30 sequences of 4 query heads
+// behind 4320 tokens, 4 partitions 41.9 / 43.6, 8 33.2 / 36.7, 16 30.9 / 33.1; one layer, 2
+// behind 8192, 12 of them 27.1 / 27.3, 16 25.7 / 24.5, 32 27.5 / 20.7.
+constexpr uint32_t kPrefixJoined = 12;
+
+inline bool prefix_joins(uint32_t parts)
+{
+    return parts <= kPrefixJoined;
+}
+
 // How the prefix of a call is cut: wavefronts of a workgroup that split the
 // rows, workgroups that share a partition, partitions; and about how long that
 // takes.
@@ -544,19 +559,21 @@ struct PrefixCut {
 // written and read again.  What a cut takes was measured for 31 shapes (1 to 33
 // layers, 4 to 32 heads, 6 to 512 rows, prefixes of 128 to 16384 tokens, 1 to 64
 // partitions) and is, in rounds of 512 workgroups, beyond what all cuts take,
-//     3 us + tiles of a partition x 1.4 us (x 1.6 with two a CU) + 0.35 ns a record,
-// for head_dim 128: the partitions that this puts first were within 1.2% of the
-// best ones on average, 7.9% at most (8 heads, 512 rows, 8192 tokens: 1 partition
-// 207 us, 4 68, 8 49, 12 52, 32 69).
-constexpr int64_t kPrefixStartNs = 3000, kPrefixTileNs = 1400;
+//     2 us + tiles of a partition x 1.2 us (x 1.5 with two a CU) + 0.2 ns a record
+//     + 0.4 us a partition where they are joined at once, 5 us where they are not,
+// for head_dim 128: the partitions that this puts first were within 0.8% of the
+// best ones on average, 9% at most (8 heads, 512 rows, 8192 tokens: 1 partition
+// 204 us, 4 65, 8 47, 12 53, 32 69).
+constexpr int64_t kPrefixStartNs = 2000, kPrefixTileNs = 1200, kPrefixJoinNs = 400, kPrefixApartNs = 5000;
 constexpr uint32_t kPrefixMostParts = 128;
 
-inline int64_t prefix_cut_ns(int64_t workgroups, int64_t tiles, int64_t records, int64_t head_dim)
+inline int64_t prefix_cut_ns(int64_t workgroups, int64_t tiles, int64_t parts, int64_t records, int64_t head_dim)
 {
     const int64_t rounds = (workgroups + 511) / 512, last = workgroups - (rounds - 1) * 512;
     const int64_t work = tiles * kPrefixTileNs * (128 + head_dim) / 256;
-    return rounds * kPrefixStartNs + work * ((rounds - 1) * 16 + (last <= 256 ? 10 : 16)) / 10 +
-           records * head_dim * 35 / 12800;
+    return rounds * kPrefixStartNs + work * ((rounds - 1) * 15 + (last <= 256 ? 10 : 15)) / 10 +
+           records * head_dim * 20 / 12800 +
+           (prefix_joins(static_cast<uint32_t>(parts)) ? parts * kPrefixJoinNs : kPrefixApartNs);
 }
 
 inline PrefixCut prefix_cut(uint32_t rows, int64_t tokens, int64_t layer_heads, int64_t head_dim)
@@ -569,7 +586,7 @@ inline PrefixCut prefix_cut(uint32_t rows, int64_t tokens, int64_t layer_heads, 
     const int64_t tiles = (tokens + tile - 1) / tile, most = std::min<int64_t>(tiles, kPrefixMostParts);
     for (int64_t want = 1; want <= most; ++want) {
         const int64_t per = (tiles + want - 1) / want, parts = (tiles + per - 1) / per;
-        const int64_t ns = prefix_cut_ns(parts * layer_heads * c.chunks, per, parts * rows * layer_heads, head_dim);
+        const int64_t ns = prefix_cut_ns(parts * layer_heads * c.chunks, per, parts, parts * rows * layer_heads, head_dim);
         if (parts == want && (c.ns < 0 || ns < c.ns)) {
             c.ns = ns;
             c.parts = static_cast<uint32_t>(parts);
@@ -579,25 +596,25 @@ inline PrefixCut prefix_cut(uint32_t rows, int64_t tokens, int64_t layer_heads, 
     return c;
 }
 
-// Whether reading the prefix once pays.  It costs one launch more than plain
-// attention, and every row leaves a record of its own tokens, too.  Plain attention
-// reads the prefix for each of `members` sequences, after the first mostly out of
-// the caches: 10 to 14 TB/s where an XCD's share of the layers fits into its L2,
-// 7 to 10 else; and a workgroup of its own costs more than the quarter of one that
-// a short rest of a sequence takes.  Prefix / plain, us: one layer of 8 heads of 128
-// and 4 query heads each, 7 sequences behind 2000 tokens 17.1 / 14.8, 8 behind 8192
-// 22.7 / 31.6, 64 behind 512 21.0 / 18.0; 8 query heads each, 16 behind 2000 24.0 /
-// 22.9, 64 behind 2000 31 / 73; 8 layers, 16 behind 512 24.4 / 25.4, 8 behind 2000 27 /
-// 68; 9 layers of 32 heads, 8 behind 160 30 / 42.
+// Whether reading the prefix once pays.  It costs a launch or two more than plain
+// attention.  Plain attention reads the prefix for each of `members` sequences, after
+// the first mostly out of the caches: 10 to 14 TB/s where an XCD's share of the layers
+// fits into its L2 (head_dim 128; 8 of 64), 7 to 10 else; and a workgroup of its own
+// costs more than the quarter of one that a short rest of a sequence takes.  Every row
+// reads its record again, 0.2 ns.  Prefix / plain, us: one layer of 8 heads of 128 and 4 query heads each, 7 sequences behind 2000
+// tokens 17.7 / 14.8, 8 behind 8192 23.2 / 32.0, 64 behind 512 18.9 / 18.3; 8 query heads
+// each, 16 behind 2000 22.2 / 23.0, 64 behind 2000 28 / 73; 8 layers, 16 behind 512 21.5 /
+// 25.3, 8 behind 2000 26 / 68; 9 layers of 32 heads, 8 behind 160 26 / 41; 6 layers of 8
+// heads and 8 query heads each, 47 behind 64 22.8 / 18.4.
 inline bool prefix_pays(const PrefixCut &c, int64_t members, int64_t group, int64_t tokens, int64_t layers, int64_t heads,
                         int64_t head_dim)
 {
     const double layer_bytes = static_cast<double>(tokens) * heads * head_dim * 4;
-    const bool cached = layer_bytes * std::max<int64_t>(1, layers / 8) <= 4 << 20;
+    const bool cached = head_dim == 128 && layer_bytes * std::max<int64_t>(1, layers / 8) <= 4 << 20;
     const double workgroups = static_cast<double>(layers) * heads * members;
     const double plain_ns = layer_bytes * layers * members / (cached ? 12500. : 8500.) +
                             (workgroups >= 1024 ? 3.5 * workgroups : 0.);
-    return c.ns + 6500 + members * group * layers * heads * head_dim * 35 / 12800 < plain_ns;
+    return c.ns + 4000 + members * group * layers * heads * head_dim * 20 / 12800 < plain_ns;
 }
 
 } // namespace

@@ -87,7 +87,7 @@ def test_matches_attention(case):
     run(*setup(L, H, G, D, bs, dtype, ctx, prefix), ctx, prefix, dtype)
 
 
-# Up to 64 and more rows a KV head; one workgroup a partition and two;
+# Up to 64 and more rows a KV head; few partitions and more than 8; one workgroup a partition and two;
 # blocks of 16 tokens or a multiple, and others; prefixes that end inside a tile.
 SHARED = [
     (1, 16, 1, 128, 16, "bf16", [688 + i for i in range(30)], 43),
@@ -102,6 +102,8 @@ SHARED = [
     (2, 16, 4, 64, 16, "bf16", [720 + (i % 9) for i in range(60)], 45),
     (2, 16, 4, 64, 8, "fp16", [720 + (i % 9) for i in range(60)], 90),
     (3, 4, 4, 128, 16, "bf16", [700, 0, 699, 41, 0, 688, 687] + [688] * 60, 43),     # some share nothing, some end there
+    (1, 8, 8, 128, 16, "bf16", [3520 + (i % 50) for i in range(20)], 220),      # more partitions than are joined at a time
+    (1, 16, 2, 128, 16, "fp16", [2400 + (i % 50) for i in range(30)], 150),
 ]
 
 
@@ -120,6 +122,21 @@ def test_long_prefix_in_several_partitions():
 def test_full_batch():
     ctx = [304 + (i % 5) for i in range(256)]
     run(*setup(1, 8, 1, 64, 16, "bf16", ctx, 19), ctx, 19, "bf16", once=True)
+
+
+# as those, with more tokens behind the prefix than one partition takes
+LONG = [
+    (1, 8, 4, 128, 16, "bf16", [5000 + 997 * i for i in range(12)] + [4000, 4010, 5, 0, 3999], 250),
+    (8, 4, 4, 64, 8, "fp16", [700, 4000, 1500, 640, 2300] + [650 + i for i in range(60)], 80),
+    (4, 16, 1, 128, 16, "fp16", [1100 + 640 * i for i in range(5)] + [700] * 20, 40),
+]
+
+
+@pytest.mark.parametrize("case", LONG, ids=lambda c: f"L{c[0]}_H{c[1]}_G{c[2]}_D{c[3]}_bs{c[4]}_{c[5]}")
+def test_many_own_tokens(case):
+    print("[case]", case, flush=True)
+    L, H, G, D, bs, dtype, ctx, prefix = case
+    run(*setup(L, H, G, D, bs, dtype, ctx, prefix), ctx, prefix, dtype)
 
 
 # as those, with few tokens behind the prefix: a wavefront takes those of a KV head

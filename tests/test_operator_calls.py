@@ -117,12 +117,14 @@ def test_select_scores_only_what_has_to_be_chosen_from(call):
 
 def test_prefix_is_read_once_only_where_that_pays(call):
     many = dict(pool_args=dict(heads=16, dim=128), q_heads=16, table_stride=200)
-    short, shared, split, lone, none = call([
+    short, shared, split, lone, none, long = call([
         dict(op="prefix"), dict(op="prefix", ctx_lens=[700] * 30, prefix_blocks=43, **many),
         dict(op="prefix", ctx_lens=[3000] * 100, prefix_blocks=180, **many),
         dict(op="prefix", ctx_lens=[3000] + [40] * 29, prefix_blocks=180, **many),
-        dict(op="prefix", ctx_lens=[3000] * 30, prefix_blocks=0, **many)])
-    once = ["prefix_rows", "attn_partial_mfma", "prefix_join"]
+        dict(op="prefix", ctx_lens=[3000] * 30, prefix_blocks=0, **many),
+        dict(op="prefix", ctx_lens=[700] * 30 + [9000, 3], prefix_blocks=43, **dict(many, table_stride=600))])
+    once = ["prefix_rows", "attn_partial_mfma"]
+    assert kernels(long) == once + ["prefix_join"]
     assert kernels(short) == ["attn_partial_mfma"] and kernels(shared) == once and kernels(split) == once
     assert shared["launches"][0]["template"][2] == 2 and split["launches"][0]["template"][2] == 4
     for x in (lone, none):
@@ -131,18 +133,23 @@ def test_prefix_is_read_once_only_where_that_pays(call):
 
 def test_prefix_cases_of_the_gpu_tests_read_it_once(call):
     import test_gpu_prefix_attention as t
-    for L, H, G, D, bs, dtype, ctx, prefix in t.SHARED + t.FEW + [(*t.SHAPE, "bf16", t.CTX, t.PREFIX)]:
+    joins = set()
+    for L, H, G, D, bs, dtype, ctx, prefix in t.SHARED + t.LONG + t.FEW + [(*t.SHAPE, "bf16", t.CTX, t.PREFIX)]:
         got = call([dict(op="prefix", pool_args=dict(layers=L, blocks=2000, bs=bs, heads=H, dim=D), q_heads=H * G,
                          table_stride=max(ctx) // bs + 1, ctx_lens=ctx, prefix_blocks=prefix)])[0]
         assert got["rc"] == OK and kernels(got)[0] == "prefix_rows", (L, H, G, D, bs)
+        if (L, H, G, D, bs, dtype, ctx, prefix) in t.LONG:
+            assert kernels(got)[2] == "prefix_join"
+            joins.add(tuple(got["launches"][2]["template"]))
         if (L, H, G, D, bs, dtype, ctx, prefix) in t.FEW:
             assert got["launches"][1]["template"][3] == 2, (L, H, G, D, bs)
+    assert {j[1] for j in joins} == {1, 8}, joins
 
 
 def test_workspaces_are_those_of_the_records(call):
     """Listed blocks: a record of head_dim + 4 floats per layer, query head and
-    partition of a sequence of several.  Shared prefix: also one per layer, query
-    head, sequence and partition of the prefix, and one per own partition."""
+    partition of a sequence of several.  Shared prefix: the same of the tokens behind
+    it, and one per layer, query head, sequence and partition of the prefix."""
     a, b, c = call([dict(op="attend", ctx_lens=[9000, 3], table_stride=600, count=600), dict(op="attend"),
                     dict(op="select")])
     assert b["workspace"] == 0 and a["workspace"] > 0 and a["workspace"] % (4 * (64 + 4) * 4) == 0
@@ -150,7 +157,7 @@ def test_workspaces_are_those_of_the_records(call):
     p = call([dict(op="prefix", ctx_lens=[700] * 30, prefix_blocks=43, pool_args=dict(heads=16, dim=128), q_heads=16,
                    table_stride=60)])[0]
     records = p["workspace"] // (16 * 132 * 4)
-    assert p["workspace"] % (16 * 132 * 4) == 0 and records >= 60 and records % 30 == 0
+    assert p["workspace"] % (16 * 132 * 4) == 0 and records >= 30 and records % 30 == 0
 
 
 def test_short_sequences_take_a_wavefront_a_head(call):
