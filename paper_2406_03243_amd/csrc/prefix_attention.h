@@ -597,20 +597,21 @@ inline PrefixCut prefix_cut(uint32_t rows, int64_t tokens, int64_t layer_heads, 
 }
 
 // Whether reading the prefix once pays.  It costs a launch or two more than plain
-// attention.  Plain attention reads the prefix for each of `members` sequences, after
-// the first mostly out of the caches: 10 to 14 TB/s where an XCD's share of the layers
-// fits into its L2 (head_dim 128; 8 of 64), 7 to 10 else; and a workgroup of its own
-// costs more than the quarter of one that a short rest of a sequence takes.  Every row
-// reads its record again, 0.2 ns.  Prefix / plain, us: one layer of 8 heads of 128 and 4 query heads each, 7 sequences behind 2000
-// tokens 17.7 / 14.8, 8 behind 8192 23.2 / 32.0, 64 behind 512 18.9 / 18.3; 8 query heads
-// each, 16 behind 2000 22.2 / 23.0, 64 behind 2000 28 / 73; 8 layers, 16 behind 512 21.5 /
-// 25.3, 8 behind 2000 26 / 68; 9 layers of 32 heads, 8 behind 160 26 / 41; 6 layers of 8
-// heads and 8 query heads each, 47 behind 64 22.8 / 18.4.
+// attention, and every row reads its record again, 0.2 ns.  Plain attention reads the
+// prefix for each of `members` sequences, after the first mostly out of the caches: 10
+// to 14 TB/s where an XCD's share of the layers fits into its L2 (8 of head_dim 64 and
+// of one KV head), 7 to 10 else; and a workgroup of its own costs more than the quarter
+// of one that a short rest of a sequence takes.  Prefix / plain, us: one layer of 8
+// heads of 128 and 4 query heads each, 7 sequences behind 2000 tokens 17.7 / 14.8, 8
+// behind 8192 23.2 / 32.0, 64 behind 512 18.9 / 18.3; 8 query heads each, 16 behind 2000
+// 22.2 / 23.0, 64 behind 2000 28 / 73; 8 layers, 16 behind 512 21.5 / 25.3, 8 behind 2000
+// 26 / 68; 9 layers of 32 heads, 8 behind 160 26 / 41; 6 layers of 8 heads and 8 query
+// heads each, 47 behind 64 22.8 / 18.4; 23 layers of one head, 7 behind 2400 22 / 38.
 inline bool prefix_pays(const PrefixCut &c, int64_t members, int64_t group, int64_t tokens, int64_t layers, int64_t heads,
                         int64_t head_dim)
 {
     const double layer_bytes = static_cast<double>(tokens) * heads * head_dim * 4;
-    const bool cached = head_dim == 128 && layer_bytes * std::max<int64_t>(1, layers / 8) <= 4 << 20;
+    const bool cached = head_dim == 128 && heads > 1 && layer_bytes * std::max<int64_t>(1, layers / 8) <= 4 << 20;
     const double workgroups = static_cast<double>(layers) * heads * members;
     const double plain_ns = layer_bytes * layers * members / (cached ? 12500. : 8500.) +
                             (workgroups >= 1024 ? 3.5 * workgroups : 0.);
