@@ -399,7 +399,7 @@ constexpr float attn_weights_up(int bf16)
 //               (prefix_attention.h) computes.  A sequence of one partition joins
 //               the prefix's records with its own sums, if they are few; others
 //               leave records.
-//               40 requests, 8 layers of 32 heads, 686 MB in 120 us, 5.7 TB/s.
+//               40 requests, 8 layers of 32 heads, 697 MB in 114 us, 6.1 TB/s.
 enum AttnMode { kAttnPlain = 0, kAttnMigrating = 1, kAttnListed = 2, kAttnOwn = 3 };
 
 template <int MODE> struct AttnArgsOf { typedef AttnArgs type; };

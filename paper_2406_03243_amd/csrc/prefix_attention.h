@@ -107,7 +107,7 @@ __device__ __forceinline__ void split_weights(float p0, float p1, uint32_t *hi, 
 // rows, 16384 tokens, 206 GFLOP in 205 us, 1.0 PFLOP/s, the matrix cores busy 55% of
 // the cycles at the clock that their power leaves (about 1.9 GHz), the rest weights and reads
 // of LDS; without the loads from memory 165 us.  Few rows are bound by HBM: 8 layers of
-// 32 heads, 40 rows, 4096 tokens, 537 MB in 112 us, 4.8 TB/s with two workgroups a
+// 32 heads, 40 rows, 4096 tokens, 537 MB in 109 us, 5.0 TB/s with two workgroups a
 // CU, a tile of each on its way.  Against it were measured: a wavefront a tile of 32
 // tokens and two of them on their way (three workgroups of two wavefronts a CU) 112 to
 // 132 us, and up to 1.5 times as long where the chip is not full; tiles of 128 tokens
@@ -432,7 +432,8 @@ __global__ void __launch_bounds__(kThreads, 2) prefix_rows(const PrefixArgs a)
 }
 
 // Joins the records of the prefix and of own tokens that left some; bound by reading
-// them (40 sequences of 32 heads of 128, 8 layers, 6.5 us).  D / 4 lanes
+// them and the launch (8 sequences of 8 heads of 128 and 4 query heads each, 33 records
+// a row, 4.9 us).  D / 4 lanes
 // a row (layer, sequence, query head) and record, SUB of them side by side, each
 // with every SUB-th record, eight records' loads in flight; they meet in LDS.
 template <int D, int SUB>
