@@ -193,9 +193,10 @@ __device__ __forceinline__ double sums_of_four(const double *s, uint32_t c)
 // consecutive blocks of its row of lanes, four blocks' bounds in flight; the D / 8
 // lanes of a head add up, and each keeps the score of one block in D / 8, so that
 // scores leave as whole lines.  The bounds are read once: 12 requests of up to 65536
-// tokens, 4 layers of 8 heads of 128, 352 MB in 68 us, 5.2 TB/s, with the 64-bit
-// sums taking half of the vector unit's time (sums across lanes through LDS, and
-// without the bounds' loads a step ahead, 79 us).
+// tokens, 4 layers of 8 heads of 128, 352 MB in 66 us, 5.3 TB/s; 32 of up to 4000, 32
+// layers, 460 MB in 101, 4.5.  HBM bounds it, at what it gives for rows of 2 KiB here and
+// there: sums in 32 bits would take 3% less, more blocks a row of lanes the same (sums
+// across lanes through LDS, and without the bounds' loads a step ahead, 79 us).
 template <int BF16, int D>
 __global__ void __launch_bounds__(kThreads) score_blocks(const SelectArgs a)
 {
@@ -282,8 +283,10 @@ __global__ void __launch_bounds__(kThreads) score_blocks(const SelectArgs a)
             unpack8<BF16>(low4[u], low);
             sum[u] = 0.0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                sum[u] += p[e] * static_cast<double>(up[e]) + m[e] * static_cast<double>(low[e]);
+            for (int e = 0; e < 8; ++e) {
+                sum[u] = __fma_rn(p[e], static_cast<double>(up[e]), sum[u]);
+                sum[u] = __fma_rn(m[e], static_cast<double>(low[e]), sum[u]);
+            }
         }
         // lane c has the score of block k0 + c / (C / 4); every C blocks, or at the
         // end, the lanes that share one take it for different k0
@@ -311,31 +314,45 @@ inline uint32_t score_blocks_per_row(uint64_t work)
 
 // The parallel part of a pass of the search below: of the counts of 256 bins,
 // which one holds the need-th key from the top, and how many of it are needed.
-// Needs kThreads threads at least; the first 256 hold a bin each.
+// The T threads' first 256, or the 64 lanes of the only wavefront, hold the bins,
+// BINS each, in order from the top.
+template <int T>
 __device__ __forceinline__ void find_bin(uint32_t *bins, uint32_t *wave_sum, uint32_t *found, uint32_t need)
 {
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    uint32_t mine = 0, sum = 0;
+    constexpr uint32_t BINS = T == 64 ? 4 : 1;
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, top = 255u - BINS * threadIdx.x;
+    uint32_t bin[BINS], mine = 0, sum = 0;
     if (threadIdx.x < 256) {
-        mine = sum = bins[255u - threadIdx.x];       // from the top
+#pragma unroll
+        for (uint32_t k = 0; k < BINS; ++k) {
+            bin[k] = bins[top - k];
+            mine += bin[k];
+        }
+        sum = mine;
 #pragma unroll
         for (uint32_t d = 1; d < 64; d *= 2) {
             const uint32_t v = __shfl_up(sum, d);
             sum += lane >= d ? v : 0u;
         }
-        if (lane == 63)
+        if (T > 64 && lane == 63)
             wave_sum[wave] = sum;
     }
-    __syncthreads();
+    if (T > 64)
+        __syncthreads();
     if (threadIdx.x < 256) {
-        for (uint32_t x = 0; x < wave; ++x)
+        for (uint32_t x = 0; T > 64 && x < wave; ++x)
             sum += wave_sum[x];
-        if (sum >= need && sum - mine < need) {
-            found[0] = 255u - threadIdx.x;
-            found[1] = need - (sum - mine);          // needed of the bin
-            found[2] = mine;                         // keys in it
+        uint32_t before = sum - mine;
+#pragma unroll
+        for (uint32_t k = 0; k < BINS; ++k) {
+            if (before < need && before + bin[k] >= need) {
+                found[0] = top - k;
+                found[1] = need - before;            // needed of the bin
+                found[2] = bin[k];                   // keys in it
+            }
+            before += bin[k];
+            bins[top - k] = 0;
         }
-        bins[255u - threadIdx.x] = 0;
     }
     __syncthreads();
 }
@@ -410,8 +427,8 @@ __global__ void __launch_bounds__(T) list_blocks(const SelectArgs a)
                 f(j, key_of(j));
         }
     };
-    if (threadIdx.x < 256)
-        bins[threadIdx.x] = 0;
+    for (uint32_t k = threadIdx.x; k < 256u; k += T)
+        bins[k] = 0;
     __syncthreads();
     uint64_t prefix = 0;
     uint32_t need = a.count;           // of the keys that begin with prefix, these many are listed
@@ -438,7 +455,7 @@ __global__ void __launch_bounds__(T) list_blocks(const SelectArgs a)
                 atomicAdd(&bins[bin], 1u);
         });
         __syncthreads();
-        find_bin(bins, wave_sum, found, need);
+        find_bin<T>(bins, wave_sum, found, need);
         prefix = prefix << 8 | found[0];
         need = found[1];
         ties = found[1] != found[2];
@@ -520,12 +537,14 @@ __global__ void __launch_bounds__(T) list_blocks(const SelectArgs a)
 
 // The kernel for rows of at most `longest` blocks, and its threads.  384 rows of up
 // to 4096 blocks, 256 / 512 / 1024 threads 16.4 / 12.4 / 11.9 us; 24 of up to 563 take
-// 5.6 with 256.  More keys a thread than a row needs cost time: 5 rows of 5829 blocks, 8 /
-// 16 of them 8.9 / 12.6 us.
+// 5.6 with 256; 8192 of up to 250, 256 / 64 threads 25.1 / 13.1, 64 of them 5.6 / 5.1.
+// More keys a thread than a row needs cost time: 5 rows of 5829 blocks, 8 / 16 of them
+// 8.9 / 12.6 us.
 inline const void *list_kernel(uint32_t longest, uint32_t *threads)
 {
-    *threads = longest <= 1024 ? 256 : 1024;
-    return longest <= 1024    ? reinterpret_cast<const void *>(&list_blocks<256, 4>)
+    *threads = longest <= 256 ? 64 : longest <= 1024 ? 256 : 1024;
+    return longest <= 256     ? reinterpret_cast<const void *>(&list_blocks<64, 4>)
+           : longest <= 1024  ? reinterpret_cast<const void *>(&list_blocks<256, 4>)
            : longest <= 4096  ? reinterpret_cast<const void *>(&list_blocks<1024, 4>)
            : longest <= 8192  ? reinterpret_cast<const void *>(&list_blocks<1024, 8>)
            : longest <= 16384 ? reinterpret_cast<const void *>(&list_blocks<1024, 16>)

@@ -105,14 +105,14 @@ def test_append_goes_block_by_block_where_tokens_are_scattered(call):
 
 
 def test_select_scores_only_what_has_to_be_chosen_from(call):
-    few, many, long, longer, longish, longest = call([
-        dict(op="select", count=7, keep_first=0), dict(op="select"),
+    few, many, some, long, longer, longish, longest = call([
+        dict(op="select", count=7, keep_first=0), dict(op="select"), dict(op="select", ctx_lens=[16 * 257, 3], table_stride=300),
         dict(op="select", ctx_lens=[16 * 1025, 3], table_stride=2000), dict(op="select", ctx_lens=[16 * 4097, 3], table_stride=9000),
         dict(op="select", ctx_lens=[16 * 8193, 3], table_stride=9000),
         dict(op="select", ctx_lens=[16 * 16385, 3], table_stride=20000)])
     assert kernels(few) == ["list_blocks"] and kernels(many) == ["score_blocks", "list_blocks"]
-    assert [x["launches"][-1]["template"] for x in (many, long, longer, longish, longest)] == [[256, 4], [1024, 4], [1024, 8], [1024, 16],
-                                                                                      [1024, 0]]
+    assert [x["launches"][-1]["template"] for x in (many, some, long, longer, longish, longest)] == [
+        [64, 4], [256, 4], [1024, 4], [1024, 8], [1024, 16], [1024, 0]]
 
 
 def test_prefix_is_read_once_only_where_that_pays(call):
