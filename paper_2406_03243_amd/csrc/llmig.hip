@@ -1617,8 +1617,8 @@ int llmig_append_rotary(const llmig_pool *pool, const llmig_append_desc *d, void
         a.by_slice = divisor(slices);
         a.by_layer = divisor(groups);
         a.by_row = divisor(pairs);
-        return launch_items(d->dtype ? append_kernel<1>(slots, layers, fast) : append_kernel<0>(slots, layers, fast), &a, units * groups * slices, slices,
-                            &a.first_unit, st);
+        return launch_items(d->dtype ? append_kernel<1>(slots, layers, fast) : append_kernel<0>(slots, layers, fast), &a,
+                            units * groups * slices, slices, &a.first_unit, st);
     };
     if (rows_heads > 0) {
         a.lanes = rows_heads * pairs;

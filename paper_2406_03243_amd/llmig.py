@@ -562,7 +562,8 @@ def _type_code(dtype, what: str) -> int:
 def _device_tables(pool: Pool, tables: torch.Tensor, batch: int) -> int:
     """Checks block tables; returns their row stride.  (Here as below, a tensor
     on the CPU or on another GPU than the pool's is refused.)"""
-    if tables.dtype != torch.int32 or tables.get_device() != pool.device_index or not tables.is_contiguous() or tables.dim() != 2:
+    if tables.dtype != torch.int32 or tables.get_device() != pool.device_index or not tables.is_contiguous() or \
+            tables.dim() != 2:
         raise ValueError("tables must be a contiguous CUDA int32 [batch][stride] tensor")
     rows, stride = tables.shape
     if rows < batch:
@@ -623,7 +624,8 @@ def llmig_append_rotary(pool: Pool, k: torch.Tensor, v: torch.Tensor, tables: to
             raise ValueError("q must be a [layers][tokens][heads][head_dim] tensor and come with q_out")
         q_heads = q.shape[2]
         qp, q_layer, q_token = _token_rows(pool, q, (layers, total, q_heads, dim), "q")
-        if q_out.shape != q.shape or q_out.dtype is not dtype or q_out.get_device() != pool.device_index or not q_out.is_contiguous():
+        if q_out.shape != q.shape or q_out.dtype is not dtype or q_out.get_device() != pool.device_index or \
+                not q_out.is_contiguous():
             raise ValueError("q_out must be a contiguous CUDA tensor of q's shape and type")
         op = q_out.data_ptr()
     elif q_out is not None:

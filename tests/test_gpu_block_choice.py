@@ -10,9 +10,9 @@ import operator_cases as oc
 pytestmark = pytest.mark.gpu
 
 if torch.cuda.is_available():
-    from paper_2406_03243_amd.llmig import (Pool, decode_blocks_workspace_bytes, llmig_append_rotary,
-                                            llmig_decode_attention_blocks, llmig_key_bounds, llmig_select_blocks,
-                                            llmig_stage, select_workspace_bytes)
+    from paper_2406_03243_amd.llmig import (LlmigError, Pool, decode_blocks_workspace_bytes, llmig_append_rotary,
+                                            llmig_decode_attention_blocks, llmig_decode_attention_prefix,
+                                            llmig_key_bounds, llmig_select_blocks, llmig_stage, select_workspace_bytes)
 
 
 def make(L, H, G, D, bs, dtype, ctx, seed=2):
@@ -364,3 +364,30 @@ def test_a_decode_step_of_long_contexts():
     llmig_decode_attention_blocks(pool2, q_out, tab2.cuda(), after, lists2, scale, ws, out2)
     torch.cuda.synchronize()
     assert torch.equal(lists2, got_lists) and torch.equal(out2, got)
+
+
+def test_tensors_elsewhere_are_refused():
+    """A tensor on the CPU, or of another shape or type, never reaches a kernel."""
+    kv, q, tables, _ = make(1, 2, 2, 64, 16, "bf16", [40])
+    dev, tab, qd = kv.cuda(), tables.cuda(), q.cuda()
+    pool = pool_of(dev)
+    low = torch.zeros((2, 1, kv.shape[2], 1, 2, 64), dtype=kv.dtype, device="cuda")
+    bounds = pool_of(low)
+    lists, out = torch.zeros((1, 1, 2, 2), dtype=torch.int32, device="cuda"), torch.empty((1, 1, 4, 64), device="cuda")
+    ws = torch.empty(4096, dtype=torch.uint8, device="cuda")
+    k = torch.zeros((1, 1, 2, 64), dtype=kv.dtype, device="cuda")
+    wide = torch.zeros((1, 1, 2, 64), dtype=torch.float32, device="cuda")
+    calls = [
+        (llmig_append_rotary, (pool, k, k, tab, [40], [1], None), [(1, k.cpu()), (2, wide), (3, tables), (1, k[:, :, :1])]),
+        (llmig_key_bounds, (pool, bounds, tab, [0], [40]), [(2, tables), (2, tab.long()), (4, [40, 41])]),
+        (llmig_select_blocks, (bounds, 16, qd, tab, [40], 0, 0, ws, lists),
+         [(2, q), (3, tables), (4, [40, 3]), (7, ws.cpu()), (8, lists.cpu()), (8, lists[:, :, :1])]),
+        (llmig_decode_attention_blocks, (pool, qd, tab, [40], lists, 0.1, ws, out),
+         [(1, q), (2, tables), (3, []), (4, lists.cpu()), (4, lists.long()), (6, ws.cpu()), (7, out.cpu()), (7, out.half())]),
+        (llmig_decode_attention_prefix, (pool, qd, tab, [40], 1, 0.1, ws, out),
+         [(1, q), (2, tables), (3, [1, 2]), (6, ws.cpu()), (7, out.cpu()), (7, out[:, :, :2])])]
+    for fn, args, bad in calls:
+        for at, value in bad:
+            with pytest.raises((ValueError, LlmigError)):
+                fn(*args[:at], value, *args[at + 1:])
+    torch.cuda.synchronize()

@@ -106,7 +106,8 @@ def test_append_goes_block_by_block_where_tokens_are_scattered(call):
 
 def test_select_scores_only_what_has_to_be_chosen_from(call):
     few, many, some, long, longer, longish, longest = call([
-        dict(op="select", count=7, keep_first=0), dict(op="select"), dict(op="select", ctx_lens=[16 * 257, 3], table_stride=300),
+        dict(op="select", count=7, keep_first=0), dict(op="select"),
+        dict(op="select", ctx_lens=[16 * 257, 3], table_stride=300),
         dict(op="select", ctx_lens=[16 * 1025, 3], table_stride=2000), dict(op="select", ctx_lens=[16 * 4097, 3], table_stride=9000),
         dict(op="select", ctx_lens=[16 * 8193, 3], table_stride=9000),
         dict(op="select", ctx_lens=[16 * 16385, 3], table_stride=20000)])
