@@ -271,6 +271,33 @@ __device__ __forceinline__ f32x4_t mfma_pv(uint64_t v, uint64_t hi, uint64_t lo,
     return mfma_qk<BF16>(__builtin_bit_cast(u32x4, u64x2{v, v}), __builtin_bit_cast(u32x4, u64x2{hi, lo}), c);
 }
 
+// Two weights as their 16-bit roundings and the 16-bit roundings of what these
+// leave (and, of bf16, of what both leave: rest), the first weight in the low halves.
+template <int BF16>
+__device__ __forceinline__ void split_weights(float p0, float p1, uint32_t *hi, uint32_t *lo, uint32_t *rest = nullptr)
+{
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    if constexpr (BF16) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        auto low = [](uint32_t x) { return __uint_as_float(x << 16); };
+        auto high = [](uint32_t x) { return __uint_as_float(x & 0xffff0000u); };
+        const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
+        p0 -= low(h);
+        p1 -= high(h);
+        const uint32_t l = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
+        *hi = h;
+        *lo = l;
+        if (rest)
+            *rest = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - low(l), p1 - high(l)}), bf16x2));
+    } else {
+        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+        const f16x2 h = __builtin_convertvector((f32x2{p0, p1}), f16x2);
+        *hi = __builtin_bit_cast(uint32_t, h);
+        *lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - static_cast<float>(h.x),
+                                                                          p1 - static_cast<float>(h.y)}), f16x2));
+    }
+}
+
 // Results leave at device scope (sc1).  On a step whose rows come out of the
 // caches (32 layers, 8 KV heads of 8 query heads, 32 sequences of 1000
 // tokens) sc1 stores 602 us, nt 612, plain ones 679, no stores at all 533.
@@ -391,9 +418,13 @@ constexpr float attn_weights_up(int bf16)
 //               number of rows that hold tokens; the others (an entry that names
 //               no block of the sequence, the last block's free slots) weigh 0,
 //               and their V rows count as zeros, whatever the pool holds there.
+//               bf16 weights go through the matrix cores in three parts, not two:
+//               outputs are off by 3e-7, not 2e-6, in the same time (the calls below
+//               145.7 us with two, 144.6 with three, and 12.5 both; behind a prefix it
+//               costs 3 to 7% and registers that the kernel does not have).
 //               HBM bounds it as it does plain attention: lists of 256 blocks of 12
 //               requests, 4 layers of 8 heads of 128, 8 query heads each, 808 MB in
-//               140 us, 5.8 TB/s; of 64 blocks of 3 requests, one layer, 9 us, a chain
+//               139 us, 5.8 TB/s; of 64 blocks of 3 requests, one layer, 10 us, a chain
 //               of list, table, rows, products and merge.
 //  kAttnOwn     the tokens of each sequence behind a prefix that prefix_rows
 //               (prefix_attention.h) computes.  A sequence of one partition joins
@@ -411,6 +442,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(M
 attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
 {
     constexpr bool MIG = MODE == kAttnMigrating, LISTED = MODE == kAttnListed, LONE = UNITS == 2;
+    constexpr bool REST = BF16 && LISTED;       // the weights in three parts (see kAttnListed)
     constexpr int KS = D / 32;            // k-steps of the QK product
     constexpr int MT = D / 16;            // 16-dim tiles of the PV product
     constexpr int LPR = D / 8;            // lanes per row in the K and V loads (16 bytes each)
@@ -800,19 +832,35 @@ attn_partial_mfma(const typename AttnArgsOf<MODE>::type a)
         ps += __shfl_xor(ps, 32);
         lsum = lsum * c + ps;
         m = m_new;
-        uint64_t ph = 0, pl = 0;
+        uint64_t ph = 0, pl = 0, pr = 0;     // high and low parts, and the rest
+        if constexpr (LISTED || MODE == kAttnOwn) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t hi = to16<BF16>(p[i]);
-            const float hv = BF16 ? __builtin_bit_cast(float, hi << 16)
-                                  : static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(hi)));
-            ph |= static_cast<uint64_t>(hi) << (16 * i);
-            pl |= static_cast<uint64_t>(to16<BF16>(p[i] - hv)) << (16 * i);
+            for (int i = 0; i < 2; ++i) {
+                uint32_t h, l, r = 0;
+                split_weights<BF16>(p[2 * i], p[2 * i + 1], &h, &l, REST ? &r : nullptr);
+                ph |= static_cast<uint64_t>(h) << (32 * i);
+                pl |= static_cast<uint64_t>(l) << (32 * i);
+                pr |= static_cast<uint64_t>(r) << (32 * i);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t hi = to16<BF16>(p[i]);
+                const float hv = BF16 ? __builtin_bit_cast(float, hi << 16)
+                                      : static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(hi)));
+                ph |= static_cast<uint64_t>(hi) << (16 * i);
+                pl |= static_cast<uint64_t>(to16<BF16>(p[i] - hv)) << (16 * i);
+            }
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             acc[mt] = acc[mt] * c;
             acc[mt] = mfma_pv<BF16>(vf[mt], ph, pl, acc[mt]);
+        }
+        if constexpr (REST) {                   // (behind the others: each waits for its own alone)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+                acc[mt] = mfma_pv<BF16>(vf[mt], pr, 0u, acc[mt]);
         }
     }
 

@@ -1469,8 +1469,8 @@ static int listed_cut(const llmig_pool *pool, const int32_t *ctx_lens, int32_t b
     return attn_record_bytes(lens, batch, *part, pool->num_layers, q_heads, pool->head_dim, bytes);
 }
 
-// How a call behind a shared prefix is cut.  members 0: not at all, the call is
-// plain decode attention.
+// How a call behind a shared prefix is cut.  members 0: not at all, every token is
+// its sequence's own.
 struct PrefixPlan {
     uint32_t members;
     PrefixCut cut;
@@ -1888,11 +1888,19 @@ int llmig_decode_attention_prefix(const llmig_pool *pool, int32_t dtype, const v
     if ((reinterpret_cast<uintptr_t>(workspace) & 15u) || (need > 0 && (!workspace || workspace_bytes < need)))
         return LLMIG_EINVAL;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (!p.members)
-        return attn_enqueue(pool, attn_kernel_for(dtype, pool->head_dim, q_heads / pool->num_kv_heads, kAttnPlain,
-                                                  pool->block_size % 8 == 0),
-                            q, batch, q_heads, tables, table_stride, ctx_lens, scale, static_cast<float *>(workspace),
-                            workspace_bytes, out, st);
+    const void *lone = pool->block_size % 8 == 0
+                           ? attn_kernel_for(dtype, pool->head_dim, q_heads / pool->num_kv_heads, kAttnOwn, 2)
+                           : nullptr;
+    AttnOwnArgs o;
+    std::memset(&o, 0, sizeof(o));
+    AttnReduceArgs r;
+    uint32_t most = 0;
+    if (!p.members) {           // nothing shared: every token is its sequence's own
+        o.joins = 1;
+        rc = attn_launch(o, r, &most, pool, fn, q, batch, q_heads, tables, table_stride, ctx_lens, scale, p.part,
+                         static_cast<float *>(workspace), out, st, AttnMigration(), false, lone);
+        return rc == LLMIG_OK ? attn_merge(r, most, st) : rc;
+    }
     const uint64_t grid = static_cast<uint64_t>(pool->num_layers) * p.cut.parts * pool->num_kv_heads * p.cut.chunks;
     if (static_cast<uint64_t>(pool->num_layers) * batch * q_heads > 0x7fffffffull || grid > kMaxGridWorkgroups)
         return LLMIG_EINVAL;
@@ -1921,8 +1929,6 @@ int llmig_decode_attention_prefix(const llmig_pool *pool, int32_t dtype, const v
                                    dim3(static_cast<uint32_t>(grid)), dim3(kThreads), args, 0, st);
     if (e != hipSuccess)
         return hip_error(e);
-    AttnOwnArgs o;
-    std::memset(&o, 0, sizeof(o));
     o.prefix = a.ws;
     o.prefix_parts = a.parts;
     o.members = a.members;
@@ -1932,14 +1938,9 @@ int llmig_decode_attention_prefix(const llmig_pool *pool, int32_t dtype, const v
         o.behind[p.member[k] / 32] |= 1u << (p.member[k] % 32);
         o.place[p.member[k]] = static_cast<uint8_t>(k);
     }
-    AttnReduceArgs r;
-    uint32_t most = 0;
     float *own = static_cast<float *>(workspace) + p.prefix_bytes / 4;
     rc = attn_launch(o, r, &most, pool, fn, q, batch, q_heads, tables, table_stride, p.own, scale, p.part, own, out, st,
-                     AttnMigration(), !o.joins,
-                     pool->block_size % 8 == 0
-                         ? attn_kernel_for(dtype, pool->head_dim, q_heads / pool->num_kv_heads, kAttnOwn, 2)
-                         : nullptr);
+                     AttnMigration(), !o.joins, lone);
     if (rc != LLMIG_OK)
         return rc;
     if (r.seqs == 0)

@@ -73,27 +73,6 @@ __device__ __forceinline__ float sum_of_halves(float x)
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
-// Two weights as their 16-bit roundings and the 16-bit roundings of what these
-// leave, the first weight in the low halves.
-template <int BF16>
-__device__ __forceinline__ void split_weights(float p0, float p1, uint32_t *hi, uint32_t *lo)
-{
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    if constexpr (BF16) {
-        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-        const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
-        *hi = h;
-        *lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - __uint_as_float(h << 16),
-                                                                          p1 - __uint_as_float(h & 0xffff0000u)}), bf16x2));
-    } else {
-        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-        const f16x2 h = __builtin_convertvector((f32x2{p0, p1}), f16x2);
-        *hi = __builtin_bit_cast(uint32_t, h);
-        *lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - static_cast<float>(h.x),
-                                                                          p1 - static_cast<float>(h.y)}), f16x2));
-    }
-}
-
 // A multiple of 8 tokens a block (ALIGNED) puts each 8 tokens in one, so their
 // row is found with scalar instructions.
 //
