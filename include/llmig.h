@@ -556,8 +556,9 @@ int llmig_decode_attention_blocks(const llmig_pool *pool, int32_t dtype, const v
  * prefix_blocks blocks (a system prompt, a document, beams): the first
  * prefix_blocks entries of the table rows are the same, in every sequence that
  * is at least that long (the caller's guarantee; shorter ones share nothing and
- * may be empty).  The prefix is read once for all of them instead of once for
- * each, and its products run on the matrix cores as one of many columns.
+ * may be empty).  Where that pays (many sequences, long prefixes), the prefix is
+ * read once for all of them instead of once for each, and its products run on
+ * the matrix cores as one of many columns.
  * Results are those of llmig_decode_attention, sums in another order.
  * 0 <= prefix_blocks <= table_stride.  workspace: the size that
  * llmig_decode_attention_prefix_workspace returns for the same lengths and
