@@ -381,7 +381,8 @@ int llmig_stream_read(const void *region, int64_t bytes, int32_t passes, int32_t
  * workspaces of the returned size, or through the entry points below, give
  * equal bits.
  * Supported: NHD pools, head_dim 64 or 128, q_heads / num_kv_heads in
- * {1, 2, 4, 8, 16}, batch <= 256; else LLMIG_EINVAL.  Arithmetic in fp32. */
+ * {1, 2, 4, 8, 16}, batch <= 256, sequences of at most 2^31 - 2049 tokens whose
+ * blocks a table row holds; else LLMIG_EINVAL.  Arithmetic in fp32. */
 int llmig_decode_attention_workspace(const int32_t *ctx_lens, int32_t batch, int32_t num_layers,
                                      int32_t q_heads, int32_t head_dim, int64_t *bytes);
 int llmig_decode_attention(const llmig_pool *pool, int32_t dtype, const void *q, int32_t batch,

@@ -1123,6 +1123,15 @@ static int attn_workspace_bytes(int64_t num_layers, int64_t n_items, int64_t q_h
     return LLMIG_OK;
 }
 
+static int32_t blocks_of(int32_t tokens, int32_t block_size)
+{
+    return tokens / block_size + (tokens % block_size != 0);
+}
+
+// The most tokens of a sequence: the kernels count in 32 bits up to a
+// partition past its last token.
+constexpr int32_t kAttnMostTokens = 0x7fffffff - kPartTokens;
+
 // Checks the arguments of a decode-attention call (all but the workspace);
 // on success gives the kernel, the item count and the workspace size.
 static int attn_check(const llmig_pool *pool, int32_t dtype, const void *q, int32_t batch, int32_t q_heads,
@@ -1141,7 +1150,7 @@ static int attn_check(const llmig_pool *pool, int32_t dtype, const void *q, int3
         (reinterpret_cast<uintptr_t>(tables) & 3u))
         return LLMIG_EINVAL;
     for (int32_t b = 0; b < batch; ++b)
-        if (ctx_lens[b] < 0 || (ctx_lens[b] + pool->block_size - 1) / pool->block_size > table_stride)
+        if (ctx_lens[b] < 0 || ctx_lens[b] > kAttnMostTokens || blocks_of(ctx_lens[b], pool->block_size) > table_stride)
             return LLMIG_EINVAL;
     if (attn_item_count(ctx_lens, batch, n_items) != LLMIG_OK || *n_items > 0x7fffffffLL)
         return LLMIG_EINVAL;
@@ -1445,11 +1454,6 @@ static bool bounds_pool(const llmig_pool *bounds)
            on_current_device(bounds);
 }
 
-static int32_t blocks_of(int32_t tokens, int32_t block_size)
-{
-    return tokens / block_size + (tokens % block_size != 0);
-}
-
 // Partial results of attention over listed blocks: the virtual lengths, how
 // they are cut, and the bytes of the records.
 static int listed_cut(const llmig_pool *pool, const int32_t *ctx_lens, int32_t batch, int32_t q_heads, int32_t count,
@@ -1461,7 +1465,7 @@ static int listed_cut(const llmig_pool *pool, const int32_t *ctx_lens, int32_t b
         if (ctx_lens[b] < 0)
             return LLMIG_EINVAL;
         const int64_t n = static_cast<int64_t>(std::min(count, blocks_of(ctx_lens[b], pool->block_size))) * pool->block_size;
-        if (n > 0x7fffffffLL - 64)
+        if (n > kAttnMostTokens)
             return LLMIG_EINVAL;
         lens[b] = static_cast<int32_t>(n);
     }

@@ -129,7 +129,21 @@ def prefix(pool_args=None, no_pool=False, dtype=1, q=A[1], batch=None, q_heads=4
                                              I64(max(0, n.value) - less), dev(out), None), n.value
 
 
-OPS = {f.__name__: f for f in (append, bounds, select, attend, prefix)}
+def decode(pool_args=None, q_heads=4, table_stride=8, ctx_lens=(100, 70), form="workspace"):
+    """llmig_decode_attention, its form without a workspace, or carrying a stage."""
+    c = lens(ctx_lens)
+    p = pool(**(pool_args or {}))
+    head = (p, 1, dev(A[1]), len(c), q_heads, dev(A[2]), table_stride, at(c), ctypes.c_float(0.1))
+    room = (dev(A[3]), I64(1 << 50), dev(A[5]))
+    if form == "noalloc":
+        return lib.llmig_decode_attention_noalloc(*head, dev(A[5]), None), None
+    if form == "migrate":
+        return lib.llmig_decode_attention_migrate(*head, *room, pool(**dict(pool_args or {}, at=2)), 1, dev(A[6]), I64(0),
+                                                  I64(1), None), None
+    return lib.llmig_decode_attention(*head, *room, None), None
+
+
+OPS = {f.__name__: f for f in (append, bounds, select, attend, prefix, decode)}
 
 
 def main():

@@ -172,3 +172,27 @@ def test_short_sequences_take_a_wavefront_a_head(call):
     assert all(x["rc"] == OK for x in got)
     kind = [[l["template"][3] for l in x["launches"] if l["kernel"] == "attn_partial_mfma"] for x in got]
     assert kind == [[1], [2], [1], [1], [0], [2]]
+
+
+@pytest.mark.parametrize("tokens", [2 ** 31 - 1, 2 ** 31 - 15, 2 ** 31 - 2048, 2 ** 31 - 2049])
+@pytest.mark.parametrize("kw", [dict(op="attend"), dict(op="prefix"), dict(op="prefix", prefix_blocks=0), dict(op="bounds"),
+                                dict(op="select")] + [dict(op="decode", form=f) for f in ("workspace", "noalloc", "migrate")],
+                         ids=lambda c: "_".join(str(x) for x in c.values()))
+def test_lengths_near_the_end_of_32_bits_need_their_blocks(call, kw, tokens):
+    """A sequence whose length rounds up to blocks past 2^31 is one the table row is too short for."""
+    good, bad = call([dict(kw), dict(kw, ctx_lens=[tokens, 70])])
+    assert good["rc"] == OK and good["launches"]
+    assert bad["rc"] == EINVAL and not bad["launches"]
+
+
+def test_longest_sequences_of_decode_attention(call):
+    """2^31 - 2049 tokens, a row of blocks for all of them; more are refused whatever the row holds."""
+    n, row = 2 ** 31 - 2049, dict(table_stride=2 ** 31 - 1, pool_args=dict(bs=1))
+    ops = [dict(op="attend", count=7), dict(op="prefix", prefix_blocks=0), dict(op="decode")]
+    for c in ops:
+        good, bad = call([dict(c, **row, ctx_lens=[n, 70]), dict(c, **row, ctx_lens=[n + 1, 70])])
+        assert good["rc"] == OK and good["launches"], c
+        assert bad["rc"] == EINVAL and not bad["launches"], c
+    wide = dict(op="attend", pool_args=dict(bs=1 << 16), table_stride=1 << 15, ctx_lens=[n, 70])
+    few, all_of_them = call([dict(wide, count=100), dict(wide, count=1 << 15)])
+    assert few["rc"] == OK and all_of_them["rc"] == EINVAL and not all_of_them["launches"]
