@@ -462,7 +462,8 @@ int llmig_decode_attention_noalloc(const llmig_pool *pool, int32_t dtype, const 
  * ids the caller guarantees in range (an id outside the pool is never written
  * to), host arrays of lengths that may be reused as soon as the call returns.
  * They allocate nothing, so they may be captured into a HIP graph (with the
- * lengths of the captured call).  Results do not change from call to call.
+ * lengths of the captured call).  Results do not change from call to call, given
+ * what the calls below leave to the caller's guarantee.
  * ------------------------------------------------------------------------- */
 
 /* New tokens of a batch.  Sequence b appends n_toks[b] tokens (0 is allowed) at
@@ -506,10 +507,12 @@ int llmig_append_rotary(const llmig_pool *pool, const llmig_append_desc *desc, v
  * the same layers, blocks, heads, head_dim and type and of block_size 1: its K
  * tiles hold the least, its V tiles the largest values, block by block, so
  * llmig_stage, llmig_pack and llmig_unpack migrate them with the cache's own
- * block maps.  A NaN key makes its two bounds NaN.  Blocks that other sequences
- * of the call update as well (a shared prefix) get the same values from each
- * that holds all of their tokens.  Both pools NHD, head_dim % 8 == 0; 0 <=
- * from_toks[b] <= ctx_lens[b]; else LLMIG_EINVAL. */
+ * block maps.  A NaN key makes its two bounds NaN.  Sequences of the call may
+ * bring the same block up to date (a shared prefix) if they hold the same
+ * number of its tokens: all of a whole block, or as many of a last, partly
+ * filled one (the caller's guarantee; else the bounds are those of any one of
+ * them).  Both pools NHD, head_dim % 8 == 0; 0 <= from_toks[b] <= ctx_lens[b];
+ * else LLMIG_EINVAL. */
 int llmig_key_bounds(const llmig_pool *pool, const llmig_pool *bounds, int32_t dtype, int32_t batch,
                      const int32_t *tables, int32_t table_stride, const int32_t *from_toks,
                      const int32_t *ctx_lens, void *stream);

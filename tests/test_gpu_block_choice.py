@@ -80,6 +80,36 @@ def test_bounds_of_nonfinite_keys(at):
     assert torch.equal(hi[rest], rows.amax(0)[rest])
 
 
+# sequences of one group share their first blocks: `common` tokens of them
+@pytest.mark.parametrize("L,H,D,bs,common,ctx,first,group", [
+    (1, 8, 128, 16, 32, [50, 40, 33, 32], [0] * 4, [0] * 4),              # whole blocks, then their own
+    (3, 16, 128, 16, 40, [40] * 5, [39, 0, 32, 40, 17], [0] * 5),         # and a partly filled one, all as far
+    (2, 40, 128, 8, 12, [12] * 3, [8, 11, 0], [0] * 3),
+    (5, 2, 64, 16, 32, [35 + i % 13 for i in range(30)], [i % 33 for i in range(30)], [i % 3 for i in range(30)]),
+    (2, 1, 8, 4, 7, [7] * 200, [4 + i % 3 for i in range(200)], [i % 9 for i in range(200)]),
+    (1, 13, 64, 12, 24, [30, 24, 34, 26], [24, 0, 0, 25], [0, 0, 1, 1])])
+def test_bounds_of_shared_blocks(L, H, D, bs, common, ctx, first, group):
+    print("[case]", L, H, D, bs, ctx, first, flush=True)
+    kv, _, tables, gen = make(L, H, 1, D, bs, "bf16", ctx)
+    for b, g in enumerate(group):
+        tables[b, :-(-common // bs)] = tables[group.index(g), :-(-common // bs)]
+    held = torch.zeros(kv.shape[2:4], dtype=torch.bool)
+    for b, n in enumerate(ctx):
+        held[oc.rows_of(tables, b, range(n), bs)] = True
+    kv[0][:, ~held] = float("nan")
+    want = torch.full((2, L, kv.shape[2], 1, H, D), 3.0, dtype=kv.dtype)
+    for b, n in enumerate(ctx):
+        for j in range(first[b] // bs, -(-n // bs)) if first[b] < n else ():
+            rows = kv[0, :, tables[b, j].long(), :min(bs, n - j * bs)]
+            want[0, :, tables[b, j].long(), 0], want[1, :, tables[b, j].long(), 0] = rows.amin(1), rows.amax(1)
+    dev, tab = kv.cuda(), tables.cuda()
+    for _ in range(3):
+        bounds = torch.full(want.shape, 3.0, dtype=kv.dtype, device="cuda")
+        llmig_key_bounds(pool_of(dev), pool_of(bounds), tab, first, ctx)
+        torch.cuda.synchronize()
+        assert torch.equal(bounds.cpu(), want)
+
+
 # ---- choice -------------------------------------------------------------------
 
 def choose(bounds, q, tables, ctx, bs, first, last, count):
