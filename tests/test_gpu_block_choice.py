@@ -110,6 +110,30 @@ def test_bounds_of_shared_blocks(L, H, D, bs, common, ctx, first, group):
         assert torch.equal(bounds.cpu(), want)
 
 
+@pytest.mark.parametrize("L,H,D,bs,ctx", [(2, 8, 128, 16, [40, 33]), (3, 2, 64, 16, [90, 40, 70]), (1, 40, 128, 4, [9, 8])])
+def test_bounds_of_ids_outside_the_pool(L, H, D, bs, ctx):
+    """An id that is not a block's is never written to; other blocks get their bounds."""
+    kv, _, tables, _ = make(L, H, 1, D, bs, "bf16", ctx)
+    nb = kv.shape[2]
+    right = tables.clone()
+    bad = {(0, 0): -1, (0, 1): nb, (1, 1): 2 ** 31 - 1, (1, 0): -2 ** 31}
+    for (b, j), x in bad.items():
+        tables[b, j] = x
+    dev = kv.cuda()
+    flat = torch.full((2 * L * nb * H * D + 4096,), 3.0, dtype=kv.dtype, device="cuda")
+    bounds = flat[2048:-2048].view(2, L, nb, 1, H, D)
+    want = bounds.cpu().clone()
+    for b, n in enumerate(ctx):
+        for j in range(-(-n // bs)):
+            if (b, j) not in bad:
+                rows = kv[0, :, right[b, j].long(), :min(bs, n - j * bs)]
+                want[0, :, right[b, j].long(), 0], want[1, :, right[b, j].long(), 0] = rows.amin(1), rows.amax(1)
+    llmig_key_bounds(pool_of(dev), pool_of(bounds), tables.cuda(), [0] * len(ctx), ctx)
+    torch.cuda.synchronize()
+    assert torch.equal(bounds.cpu(), want) and torch.equal(dev.cpu(), kv)
+    assert bool((flat[:2048] == 3).all()) and bool((flat[-2048:] == 3).all())
+
+
 # ---- choice -------------------------------------------------------------------
 
 def choose(bounds, q, tables, ctx, bs, first, last, count):
