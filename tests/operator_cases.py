@@ -128,3 +128,88 @@ def worst(got, want, tol):
     ratio = torch.where(tol > 0, err / tol.clamp(min=1e-300), torch.where(err > 0, math.inf, 0.0))
     ratio = torch.where(torch.isfinite(got), ratio, torch.tensor(math.inf, dtype=torch.float64))
     return float(ratio.max()) if ratio.numel() else 0.0
+
+
+# ---- inputs whose scores are exact --------------------------------------------------
+# All keys and values are 0 but those of a few live tokens, whose keys are -1 in
+# the first dim and whose values are of one sign; queries are x in the first dim
+# alone, the scale is 1.  So scores are 0 and -x, exactly, every group of 16 tokens
+# has the largest among them, sums of the others' weights are whole numbers, and
+# what is left of a row's error is that of the live tokens' weights w = exp(-x):
+#   the scaled score and what is taken from it, |x| <= 2: (5.8 + 4) u ln 2, and the
+#   exponential's ulp, 2 u: 9 u; of two live tokens at most 2 * 3 parts added to others,
+#   2 u each: 12 u; 2 live weights, and 14 binades that the weight sum can pass: 16
+#   u; division, factors between wavefronts and partitions (all 1): 4 u; 41 u in all,
+# and the parts that a weight is split into (a part is off by half a step of what it
+# rounds): 2^-22 of fp16's two and of bf16's three, 2^-17 of bf16's two.
+CHAIN = 41 * U32
+PARTS = {("fp16", 2): 2.0 ** -22, ("bf16", 2): 2.0 ** -17, ("bf16", 3): 2.0 ** -22}
+
+
+def split(w, dtype, parts):
+    """w (float64) as the sum of `parts` roundings to the type, each of what the
+    ones before leave; fp16 takes it times 2^7."""
+    t, up = TYPES[dtype], 128.0 if dtype == "fp16" else 1.0
+    left, total = (w * up).float(), torch.zeros_like(w)
+    for _ in range(parts):
+        part = left.to(t).float()
+        left, total = left - part, total + part.double()
+    return total / up
+
+
+def telling(dtype, parts):
+    """16 queries x whose weights lose most with one part less than `parts`."""
+    x = torch.arange(0.25, 2.0, 2.0 ** -7, dtype=torch.float64).to(TYPES[dtype]).double().unique()
+    w = torch.exp(-x)
+    loss = (split(w, dtype, parts - 1) / w - 1).abs()
+    return x[loss.argsort(descending=True)[:16]]
+
+
+def exact_scores(kv, q, tables, live, dtype, parts):
+    """Fills kv and q; live: (sequence, token) pairs, at most two of a sequence's."""
+    bs, D = kv.shape[3], kv.shape[5]
+    x = telling(dtype, parts)
+    kv.zero_()
+    q.zero_()
+    rows = torch.arange(q[..., 0].numel()).view(q.shape[:3])
+    q[..., 0] = x[rows * 5 % 16].to(q.dtype)
+    v = (1.0 + torch.arange(D) % 8 / 8).to(kv.dtype)
+    for b, t in live:
+        blk, slot = int(tables[b, t // bs]), t % bs
+        kv[0, :, blk, slot, :, 0] = -1
+        kv[1, :, blk, slot] = v
+
+
+def tiny_weights(n):
+    """What a row of small_weights() comes to, and its bound: the score -10.6 is one
+    product and exact, so a weight is off by what scaling it and taking the largest
+    from it round, 15.3 (1 + 1 + 1) u ln 2, and the exponential's 2 u, 34 u, or, of a
+    partition without the first token, by what the factor does to which its maximum
+    goes through a record, 15.3 (2 + 1 + 1) u ln 2 + 2 u = 44 u; its two parts by 2^-32 of
+    the largest; the sums as in attention()."""
+    w = (n - 1) * math.exp(float(torch.tensor(-10.6, dtype=torch.float16)))
+    return w / (1 + w), n * 2.0 ** -32 + w / (1 + w) * U32 * (44 + 4 + LAMBDA * 2 * math.sqrt(64 + -(-n // 16)))
+
+
+def exact_rows(q, D, ctx, live):
+    """The 64-bit outputs for inputs of exact_scores(); live: how many live tokens each sequence attends to."""
+    w = torch.exp(-q[..., :1].double())
+    k, n = (torch.tensor(x, dtype=torch.float64)[None, :, None, None] for x in (live, ctx))
+    v = 1.0 + torch.arange(D, dtype=torch.float64) % 8 / 8
+    return k * w * v / torch.clamp(n - k + k * w, min=1e-9)
+
+
+def check_exact(out, q, ctx, live, dtype, parts):
+    """The largest error of outputs of such inputs, in bounds."""
+    want = exact_rows(q, q.shape[3], ctx, live)
+    return worst(out, want, want * (PARTS[dtype, parts] + CHAIN))
+
+
+def guarded(shape, dtype, value, device="cuda"):
+    """(a tensor of `shape` inside a buffer filled with `value`, a check that nothing around it changed)."""
+    n = math.prod(shape)
+    flat = torch.full((n + 8192,), value, dtype=dtype, device=device)
+
+    def untouched():
+        return bool((flat[:4096] == value).all()) and bool((flat[4096 + n:] == value).all())
+    return flat[4096:4096 + n].view(shape), untouched
