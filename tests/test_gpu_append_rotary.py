@@ -224,3 +224,24 @@ def test_ids_outside_the_pool_are_not_written():
     want = torch.zeros_like(kv)
     want[:, 0, 2, 0] = 1
     assert torch.equal(kv, want)
+
+
+@pytest.mark.parametrize("layouts", [(0, 0), (1, 1), (2, 3), (3, 2)])
+@pytest.mark.parametrize("L,H,G,D,news", [(1, 2, 3, 64, [1, 1]), (3, 8, 1, 128, [300, 129]), (2, 13, 1, 104, [400, 2])])
+def test_nothing_is_written_around_pool_and_queries(layouts, L, H, G, D, news):
+    print("[case]", layouts, L, H, G, D, news, flush=True)
+    bs, n, froms = 16, sum(news), [5, 0]
+    need = [-(-(f + a) // bs) for f, a in zip(froms, news)]
+    nb = sum(need)
+    tables = torch.zeros((2, max(need)), dtype=torch.int32)
+    tables[0, :need[0]], tables[1, :need[1]] = torch.arange(need[0]), torch.arange(need[0], nb)
+    kv, whole = oc.guarded((2, L, nb, bs, H, D), torch.bfloat16, 3.0)
+    q_out, q_whole = oc.guarded((L, n, H * G, D), torch.bfloat16, 5.0)
+    x = torch.randn((L, n, H * (G + 2), D), generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).cuda()
+    llmig_append_rotary(Pool(list(kv[0].unbind(0)), list(kv[1].unbind(0)), layouts), x[:, :, H * G:H * (G + 1)],
+                        x[:, :, H * (G + 1):], tables.cuda(), froms, news, table_of(512, D).cuda(), q=x[:, :, :H * G], q_out=q_out)
+    torch.cuda.synchronize()
+    assert whole() and q_whole()
+    assert int((q_out == 5).sum()) < q_out.numel() // 1000 + 10
+    written = (kv != 3).view(2, -1).sum(1)
+    assert bool((written <= L * n * H * D).all()) and bool((written > L * n * H * D * 0.999 - 10).all())

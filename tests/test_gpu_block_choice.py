@@ -445,3 +445,37 @@ def test_tensors_elsewhere_are_refused():
             with pytest.raises((ValueError, LlmigError)):
                 fn(*args[:at], value, *args[at + 1:])
     torch.cuda.synchronize()
+
+
+# ---- fp16 rows of 128, and what stands around the outputs -----------------------------
+
+@pytest.mark.parametrize("order,holes", [("ascending", False), ("last", False), ("any", True)])
+@pytest.mark.parametrize("L,H,G,D,bs,ctx,count", [
+    (2, 2, 4, 128, 16, [300, 45, 0, 17], 5), (1, 1, 16, 128, 4, [203], 13), (1, 1, 2, 128, 16, [9000], 200),
+    (1, 2, 1, 128, 24, [1000, 990], 30), (1, 8, 8, 128, 16, [3001, 2500, 40], 64), (4, 3, 2, 128, 8, [700, 650], 70)])
+def test_attention_over_lists_of_fp16_rows(order, holes, L, H, G, D, bs, ctx, count):
+    print("[case]", order, L, H, G, D, bs, ctx, count, flush=True)
+    kv, q, tables, gen = make(L, H, G, D, bs, "fp16", ctx)
+    attend(kv, q, tables, ctx, some_lists(L, len(ctx), H, count, ctx, bs, gen, order, holes), "fp16")
+
+
+# rows that are listed whole, and lists of each kernel (one wavefront, four, sixteen; keys in registers or not)
+@pytest.mark.parametrize("D,bs,ctx,count", [
+    (64, 16, [40, 0, 17], 7), (128, 16, [600, 33], 3), (64, 16, [4000, 100], 61), (64, 4, [4097], 129), (64, 1, [5000], 77),
+    (128, 1, [9001, 5], 301), (64, 1, [17000, 16385], 1000)])
+def test_nothing_is_written_around_the_lists(D, bs, ctx, count):
+    print("[case]", D, bs, ctx, count, flush=True)
+    kv, q, tables, gen = make(2, 3, 2, D, bs, "bf16", ctx)
+    b = random_bounds(kv, gen)
+    dev = b.cuda()
+    pool = pool_of(dev)
+    ws, ws_whole = oc.guarded((select_workspace_bytes(pool, bs, ctx),), torch.uint8, 0xFF)
+    blocks, whole = oc.guarded((2, len(ctx), 3, count), torch.int32, -9)
+    llmig_select_blocks(pool, bs, q.cuda(), tables.cuda(), ctx, 0, 1, ws, blocks)
+    torch.cuda.synchronize()
+    assert whole() and ws_whole() and torch.equal(dev.cpu(), b)
+    for x in range(len(ctx)):
+        n = -(-ctx[x] // bs)
+        ids = tables[x, :n].long()
+        for l in range(2):
+            assert torch.equal(blocks[l, x].cpu(), oc.select(b[0, l, ids, 0], b[1, l, ids, 0], q[l, x], n, 0, 1, count))
