@@ -28,6 +28,49 @@ class Append(ctypes.Structure):
                 ("positions", I32), ("rotary_dim", I32), ("interleaved", I32)]
 
 
+class Divisor(ctypes.Structure):
+    _fields_ = [("d", U32), ("m", U32), ("shift", U32)]
+
+
+# The kernels' argument structures, as the sources declare them (to the last field that a test reads).
+class AppendArgs(ctypes.Structure):
+    _fields_ = [("pointers", U64 * 13), ("first_unit", U32), ("num_layers", U32), ("num_blocks", U32), ("block_size", U32),
+                ("table_stride", U32), ("tile_bytes", U32), ("q_heads", U32), ("kv_heads", U32), ("tokens", U32),
+                ("batch", U32), ("rows_heads", U32 * 3), ("row_chunks", U32), ("lanes", U32), ("half", U32),
+                ("interleaved", U32), ("wide", U32), ("layouts", I32 * 2), ("one_each", U32), ("tensor", U32),
+                ("by_slice", Divisor), ("by_layer", Divisor)]
+
+
+class BoundsArgs(ctypes.Structure):
+    _fields_ = [("pointers", U64 * 3), ("num_layers", U32), ("num_blocks", U32), ("block_size", U32), ("table_stride", U32),
+                ("tile_bytes", U32), ("batch", U32), ("slot_chunks", U32), ("rows", U32), ("side", U32), ("one_each", U32),
+                ("first_item", U32), ("by_slice", Divisor), ("by_group", Divisor)]
+
+
+class SelectArgs(ctypes.Structure):
+    _fields_ = [("pointers", U64 * 5), ("num_layers", U32), ("num_blocks", U32), ("batch", U32), ("q_heads", U32),
+                ("kv_heads", U32), ("table_stride", U32), ("keep_first", U32), ("keep_last", U32), ("count", U32),
+                ("blocks", U32), ("first_item", U32), ("per_row", U32), ("parts", U32), ("slices", U32)]
+
+
+class AttnArgs(ctypes.Structure):
+    _fields_ = [("pointers", U64 * 5), ("scale", ctypes.c_float), ("num_layers", U32), ("batch", U32), ("q_heads", U32),
+                ("kv_heads", U32), ("block_size", U32), ("table_stride", U32), ("item_base", U32), ("layer_items", U32)]
+
+
+STRUCTS = {"append_rotary_rows": AppendArgs, "append_rotary_slots": AppendArgs, "append_rotary_dims": AppendArgs,
+           "key_bounds_rows": BoundsArgs, "score_blocks": SelectArgs, "list_blocks": SelectArgs, "attn_partial_mfma": AttnArgs}
+
+
+def fields(args):
+    out = {}
+    for name, kind in args._fields_:
+        v = getattr(args, name)
+        if name != "pointers":
+            out[name] = v.d if kind is Divisor else list(v) if isinstance(v, ctypes.Array) else v
+    return out
+
+
 launches = []
 
 
@@ -36,6 +79,8 @@ def on_launch(name, gb, lds, args):
     m = re.search(r"\d+([a-z]+_[a-z_]+?)(?:I|E|N)", name.decode().split("GLOBAL__N_1")[-1])
     launches.append({"kernel": m.group(1), "grid": gb[0], "block": gb[3],
                      "template": [int(x) for x in re.findall(r"Li(\d+)E", name.decode())]})
+    if m.group(1) in STRUCTS:
+        launches[-1]["args"] = fields(STRUCTS[m.group(1)].from_address(args))
 
 
 fake = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
