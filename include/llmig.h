@@ -522,10 +522,10 @@ int llmig_key_bounds(const llmig_pool *pool, const llmig_pool *bounds, int32_t d
  * (16-byte aligned) and a sequence of n = ceil(ctx_lens[b] / block_size) blocks:
  *     score_j = sum_d P_d hi_jd + N_d lo_jd,   P_d = sum_h max(q_hd, 0),  N_d = sum_h min(q_hd, 0)
  * over the query heads h of g, the sum over them of the largest q_h . k that
- * keys within the block's bounds can have.  Sums in 64 bits; a NaN score counts
- * as +infinity.  The first keep_first and the last keep_last blocks are always
- * chosen, then those of the highest scores (of equal ones the first), `count`
- * in all, or all n where n <= count.  blocks: device int32
+ * keys within the block's bounds can have.  Sums in 64 bits, in one order for
+ * every block; a NaN score counts as +infinity.  The first keep_first and the
+ * last keep_last blocks are always chosen, then those of the highest scores (of
+ * equal ones the first), `count` in all, or all n where n <= count.  blocks: device int32
  * [num_layers][batch][num_kv_heads][count], the chosen block numbers (indexes
  * into the sequence's table row) ascending, then -1.  count >= 1 and >=
  * keep_first + keep_last; bounds as llmig_key_bounds keeps them, head_dim 64 or
@@ -547,8 +547,9 @@ int llmig_select_blocks(const llmig_pool *bounds, int32_t dtype, int32_t block_s
  * nothing, and a block named twice counts twice.  A row that names no token
  * gives zeros.  workspace: the size that
  * llmig_decode_attention_blocks_workspace returns for the same lengths, 16-byte
- * aligned.  Other arguments, limits, arithmetic and errors as
- * llmig_decode_attention. */
+ * aligned.  Arithmetic in fp32, weights as the sum of two (fp16) or three (bf16)
+ * 16-bit roundings, within 2^-22 of a weight or 2^-32 of the row's largest.
+ * Other arguments, limits and errors as llmig_decode_attention. */
 int llmig_decode_attention_blocks_workspace(const llmig_pool *pool, const int32_t *ctx_lens, int32_t batch,
                                             int32_t q_heads, int32_t count, int64_t *bytes);
 int llmig_decode_attention_blocks(const llmig_pool *pool, int32_t dtype, const void *q, int32_t batch,
@@ -563,7 +564,9 @@ int llmig_decode_attention_blocks(const llmig_pool *pool, int32_t dtype, const v
  * may be empty).  Where that pays (many sequences, long prefixes), the prefix is
  * read once for all of them instead of once for each, and its products run on
  * the matrix cores as one of many columns.
- * Results are those of llmig_decode_attention, sums in another order.
+ * Results are those of llmig_decode_attention, sums in another order; a weight
+ * is the sum of two 16-bit roundings, within 2^-17 of it (bf16), or 2^-22 of it or
+ * 2^-32 of the row's largest (fp16).
  * 0 <= prefix_blocks <= table_stride.  workspace: the size that
  * llmig_decode_attention_prefix_workspace returns for the same lengths and
  * prefix, 16-byte aligned.  Other arguments, limits and errors as

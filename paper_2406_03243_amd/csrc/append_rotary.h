@@ -357,8 +357,9 @@ __global__ void __launch_bounds__(kThreads) append_rotary_slots(const AppendArgs
 // HDN.  Unit: (block, layer); a lane turns 8 dims of 8 slots round in
 // registers, and LDS puts the lanes' pieces in the tile's order, so that a
 // wavefront stores whole KiB.  Slots that the call does not write keep theirs.
-// Values of the call above, 757 MB in 152 us, 5.0 TB/s; LDS holds four workgroups a
-// CU, and bank conflicts take 5% of the cycles.
+// Values of the call above, 757 MB in 152 us, 5.0 TB/s; a CU holds three workgroups
+// (140 registers, most of them for the rotation of eight rows of keys, which values
+// do without; its LDS would hold four), and bank conflicts take 5% of the cycles.
 template <int BF16>
 __global__ void __launch_bounds__(kThreads) append_rotary_dims(const AppendArgs a)
 {

@@ -419,9 +419,14 @@ constexpr float attn_weights_up(int bf16)
 //               no block of the sequence, the last block's free slots) weigh 0,
 //               and their V rows count as zeros, whatever the pool holds there.
 //               bf16 weights go through the matrix cores in three parts, not two:
-//               outputs are off by 3e-7, not 2e-6, in the same time (the calls below
-//               145.7 us with two, 144.6 with three, and 12.5 both; behind a prefix it
-//               costs 3 to 7% and registers that the kernel does not have).
+//               outputs whose scores are exact are off by 3e-7 at most, not 6e-6, in
+//               the same time (the calls below 145.7 us with two, 144.6 with three, and
+//               12.5 both; behind a prefix it costs 3 to 7% and registers that the
+//               kernel does not have).  fp16 (two parts) takes what bf16 takes, 143.8
+//               against 142.6 us, 67.7 against 66.2 for 60 lists of up to 400 tokens of
+//               8 layers, although with head_dim 128 and UNITS its kernels want one to
+//               three registers more than four wavefronts a SIMD have and keep 8 (UNITS
+//               2: 16) bytes a lane in scratch memory.
 //               HBM bounds it as it does plain attention: lists of 256 blocks of 12
 //               requests, 4 layers of 8 heads of 128, 8 query heads each, 808 MB in
 //               139 us, 5.8 TB/s; of 64 blocks of 3 requests, one layer, 10 us, a chain

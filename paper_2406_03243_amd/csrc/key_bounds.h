@@ -8,9 +8,10 @@
 // Score of a block for a KV head's group of query heads: the sum of that bound
 // over the group, one product with P = sum_h max(q_h, 0), N = sum_h min(q_h, 0):
 //     score_j = sum_d P_d hi_jd + N_d lo_jd.
-// Scores are compared with each other, so they are summed in 64 bits: products
-// of 16-bit values are exact there, and which block is listed does not hang on
-// the order of a sum.
+// Scores are compared with each other, so they are summed in 64 bits, in one order
+// for every block: equal bounds give equal scores, and a call's choice repeats.
+// (The sum is exact where its terms span few enough exponents for 53 bits; else
+// blocks whose scores differ by its rounding may change places.)
 #pragma once
 
 #include "append_rotary.h"

@@ -584,7 +584,7 @@ inline PrefixCut prefix_cut(uint32_t rows, int64_t tokens, int64_t layer_heads, 
 // of one that a short rest of a sequence takes.  Prefix / plain, us: one layer of 8
 // heads of 128 and 4 query heads each, 7 sequences behind 2000 tokens 17.7 / 14.8, 8
 // behind 8192 23.2 / 32.0, 64 behind 512 18.9 / 18.3; 8 query heads each, 16 behind 2000
-// 22.2 / 23.0, 64 behind 2000 28 / 73; 8 layers, 16 behind 512 21.5 / 25.3, 8 behind 2000
+// 22.2 / 23.0 (the rule takes the latter here), 64 behind 2000 28 / 73; 8 layers, 16 behind 512 21.5 / 25.3, 8 behind 2000
 // 26 / 68; 9 layers of 32 heads, 8 behind 160 26 / 41; 6 layers of 8 heads and 8 query
 // heads each, 47 behind 64 22.8 / 18.4; 23 layers of one head, 7 behind 2400 22 / 38.
 inline bool prefix_pays(const PrefixCut &c, int64_t members, int64_t group, int64_t tokens, int64_t layers, int64_t heads,
